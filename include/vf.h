@@ -336,6 +336,132 @@ int vf_gemm_noalloc(const void* A, int64_t lda, const void* B, int64_t ldb, floa
                     int32_t N, int32_t K, float alpha, int32_t accumulate, int32_t nsplit,
                     void* stream);
 
+/* ---- operators between an attention block's projections, callable on their own --------------
+ * What stands between the projections of a block (vf_gemm) when positions turn the queries and
+ * keys instead of being added to the input, heads are normalised, and the keys and values come
+ * from a sequence of another length (an encoder read by a decoder; with equal lengths the
+ * encoder's own self-attention).  All are functions of the rows of one virtual node: nothing
+ * crosses rows of different samples.
+ *
+ * Conventions of these entry points, beside those at the top of this file
+ *   - a tensor [rows, heads, d_head] or [batch, rows, heads, d_head] is given by a pointer and its
+ *     strides in ELEMENTS; the elements of a head are contiguous.  Input strides may be any (0 repeats
+ *     a row or head), output strides must keep the outputs apart;
+ *   - device memory is on the current device; work is enqueued on `stream` (NULL = the default
+ *     stream), nothing is allocated, nothing synchronises, and no state is kept between calls, so
+ *     calls on different streams do not disturb each other as long as each has its own workspace.
+ *     Calls may be captured into a HIP graph; a workspace belongs to the graph then;
+ *   - the results of a call do not depend on what runs beside it: sums are taken in a fixed order,
+ *     without atomics;
+ *   - a call over no rows is a no-op (gradients that sum over the rows are then 0);
+ *   - VF_EINVAL, with nothing enqueued, for malformed arguments. */
+
+/* Which elements of a head turn together: the leading rot_dim elements form rot_dim / 2 pairs. */
+#define VF_ROPE_HALF         0   /* element j with element j + rot_dim / 2 */
+#define VF_ROPE_INTERLEAVED  1   /* element 2 j with element 2 j + 1 */
+
+/* How the pairs' frequencies f_j = base^(-2 j / rot_dim) are changed for contexts longer than trained on. */
+#define VF_ROPE_PLAIN   0        /* not at all */
+#define VF_ROPE_LINEAR  1        /* f_j / factor: positions move closer together */
+#define VF_ROPE_PARTS   2        /* by how often a pair turns over the trained length, r_j = trained_len f_j / 2 pi: pairs with
+                                    r_j >= beta_fast keep f_j, with r_j <= beta_slow have f_j / factor, between them
+                                    the two are mixed in proportion to r_j */
+
+#define VF_ROPE_MAX_PAIRS 128
+
+/* Plain data, filled by vf_rope_make, read on the host by every call it is given to. */
+typedef struct vf_rope_plan {
+  int32_t layout;                    /* VF_ROPE_HALF | VF_ROPE_INTERLEAVED */
+  int32_t rot_dim;                   /* even, 2 .. 2 VF_ROPE_MAX_PAIRS */
+  float   scale;                     /* factor of every cosine and sine */
+  float   reserved;
+  double  turns[VF_ROPE_MAX_PAIRS];  /* whole turns per position of pair j: f_j / (2 pi) */
+} vf_rope_plan;
+
+/* Fills a plan; host only.  base > 1; LINEAR: factor > 0; PARTS: factor > 0, trained_len > 0 and
+ * beta_fast > beta_slow (ignored otherwise); scale: factor of cosine and sine (1 normally). */
+int vf_rope_make(int32_t layout, int32_t rot_dim, double base, int32_t scaling, double factor,
+                 int64_t trained_len, double beta_fast, double beta_slow, double scale,
+                 vf_rope_plan* out);
+
+/* Turns heads by their rows' positions.  x, y: [rows, heads, d_head], dtype VF_F32 or VF_BF16; pair
+ * (a, b) of a row at position p becomes  s (a cos t - b sin t), s (b cos t + a sin t)  with the angle
+ * t = 2 pi p turns[j] (reduced in float64: exact for far positions) and the plan's scale s;
+ * elements from rot_dim on are copied.  inverse != 0 turns by -t: with the same scale that is the
+ * operator's backward pass (dx from dy).  positions: device int32 [rows], or NULL for
+ * first + (seq_len > 0 ? row % seq_len : row).  d_head: rot_dim .. 512.  y may be x (same strides). */
+int vf_rope(int32_t dtype, const void* x, int64_t x_row, int64_t x_head, void* y, int64_t y_row,
+            int64_t y_head, int64_t rows, int32_t heads, int32_t d_head, const int32_t* positions,
+            int64_t first, int64_t seq_len, const vf_rope_plan* plan, int32_t inverse, void* stream);
+
+/* RMS norm of every head and the rotation in one pass:  y = R(x rstd gamma),
+ * rstd = (mean over the head of x^2 + eps)^(-1/2), rounded once.  x, y: [rows, q_heads + k_heads, d_head] (as the
+ * projection writes them side by side; either number may be 0 for tensors of their own).
+ * gamma_q, gamma_k: device fp32 [d_head], the weights of the first q_heads and the last k_heads heads
+ * (NULL = all ones).  plan: NULL = the norm alone.  Positions as in vf_rope.  y may be x. */
+int vf_qk_norm_rope(int32_t dtype, const void* x, int64_t x_row, int64_t x_head, void* y, int64_t y_row,
+                    int64_t y_head, int64_t rows, int32_t q_heads, int32_t k_heads, int32_t d_head,
+                    const float* gamma_q, const float* gamma_k, float eps, const int32_t* positions,
+                    int64_t first, int64_t seq_len, const vf_rope_plan* plan, void* stream);
+
+/* Its backward pass.  x as given to the forward pass, dy the gradient at y:  with g = R^T dy and
+ * xhat = x rstd,  dx = rstd (g gamma - xhat mean(g gamma xhat)),
+ * dgamma = alpha sum_{rows, heads} g xhat (+ dgamma if accumulate != 0) -- alpha = b_i/B and accumulate fold a node's
+ * gradient into the gradient buffer, as in vf_gemm.  dgamma_q, dgamma_k: device fp32 [d_head] or NULL
+ * (not wanted).  dx may be x or dy (same strides).  workspace: device, 16-byte aligned, of at least
+ * vf_qk_norm_rope_workspace bytes (0 where no dgamma is wanted). */
+int vf_qk_norm_rope_backward(int32_t dtype, const void* x, int64_t x_row, int64_t x_head, const void* dy,
+                             int64_t dy_row, int64_t dy_head, void* dx, int64_t dx_row, int64_t dx_head,
+                             int64_t rows, int32_t q_heads, int32_t k_heads, int32_t d_head,
+                             const float* gamma_q, const float* gamma_k, float eps,
+                             const int32_t* positions, int64_t first, int64_t seq_len,
+                             const vf_rope_plan* plan, float* dgamma_q, float* dgamma_k, float alpha,
+                             int32_t accumulate, void* workspace, int64_t workspace_bytes, void* stream);
+int64_t vf_qk_norm_rope_workspace(int64_t rows, int32_t q_heads, int32_t k_heads, int32_t d_head);
+
+/* Where a [batch, rows, heads, d_head] tensor's elements lie: strides in elements. */
+typedef struct vf_attn_layout {
+  int64_t batch, row, head;
+} vf_attn_layout;
+
+/* Attention of q_rows queries to k_rows keys and values.  Plain data, read on the host by the call.
+ * Pointers 16-byte aligned; every stride a multiple of 16 bytes; d_head a multiple of 8, 8 .. 128. */
+typedef struct vf_attn_shape {
+  int32_t dtype;                     /* VF_F32 | VF_BF16, of all tensors but lse */
+  int32_t batch, q_rows, k_rows;
+  int32_t q_heads, kv_heads;         /* q_heads a multiple of kv_heads: query head h reads key head h / (q_heads / kv_heads) */
+  int32_t d_head;
+  float   scale;                     /* > 0: factor of every product q . k (1 / sqrt(d_head) normally) */
+  vf_attn_layout q, k, v, o;         /* o: output */
+  vf_attn_layout d_o, dq, dk, dv;    /* backward only: gradient of o (input), of q, k, v (outputs) */
+} vf_attn_shape;
+
+/* o = softmax_keys(scale q k^T over the visible keys) v.
+ *   q_len     device int32 [batch] or NULL: rows from q_len[b] on are padding (values clamped into [0, q_rows])
+ *   k_len     device int32 [batch] or NULL: keys from k_len[b] on are not visible (clamped into [0, k_rows])
+ *   key_mask  device uint8 [batch, k_rows] or NULL: keys with a 0 are not visible
+ *   lse       device fp32 [batch, q_heads, q_rows] or NULL: natural logarithm of the sum of exp of a row's
+ *             visible scaled products, which the backward pass needs
+ * A row that is padding or sees no key has output 0 and lse -infinity.  What lies in padded rows and
+ * invisible keys and values, infinities and NaN among it, has no influence.  Sums and softmax are fp32; with VF_BF16
+ * the probabilities are rounded to bf16 as operands of the product with v.
+ * workspace: device, 16-byte aligned, at least vf_attention_workspace(shape, 0) bytes. */
+int vf_attention(const vf_attn_shape* shape, const void* q, const void* k, const void* v,
+                 const int32_t* q_len, const int32_t* k_len, const uint8_t* key_mask, void* o, float* lse,
+                 void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Gradients of q, k and v from d_o, the gradient of o; o and lse as the forward call wrote them, the
+ * same lengths and mask.  Gradients of padded rows and invisible keys are 0; those of shared
+ * keys and values are summed over the query heads that read them.
+ * workspace: at least vf_attention_workspace(shape, 1) bytes. */
+int vf_attention_backward(const vf_attn_shape* shape, const void* q, const void* k, const void* v,
+                          const int32_t* q_len, const int32_t* k_len, const uint8_t* key_mask,
+                          const void* o, const float* lse, const void* d_o, void* dq, void* dk, void* dv,
+                          void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Bytes of workspace of the two calls above (backward = 0 / 1); VF_EINVAL (negative) for a malformed shape. */
+int64_t vf_attention_workspace(const vf_attn_shape* shape, int32_t backward);
+
 /* ---- training state of this device (Section 4.1) ---------------------------------------
  * What a device that joins a job has to receive before it can continue the job's steps: the
  * master parameters, the optimizer state, and the state the passes themselves carry (the

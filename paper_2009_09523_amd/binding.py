@@ -12,6 +12,9 @@ VF_MLP, VF_ENCODER, VF_CONV = 0, 1, 2
 VF_F32, VF_BF16 = 0, 1
 VF_SGDM, VF_ADAM = 0, 1
 VF_MAX_DIMS = 16
+VF_ROPE_HALF, VF_ROPE_INTERLEAVED = 0, 1
+VF_ROPE_PLAIN, VF_ROPE_LINEAR, VF_ROPE_PARTS = 0, 1, 2
+VF_ROPE_MAX_PAIRS = 128
 VF_FLAG_FUSED_ACCUMULATE = 1
 VF_FLAG_NO_GRAPH = 2
 VF_FLAG_OVERLAP = 4
@@ -58,6 +61,22 @@ class VfConfig(C.Structure):
     ]
 
 
+class VfRopePlan(C.Structure):
+    _fields_ = [("layout", C.c_int32), ("rot_dim", C.c_int32), ("scale", C.c_float), ("reserved", C.c_float),
+                ("turns", C.c_double * VF_ROPE_MAX_PAIRS)]
+
+
+class VfAttnLayout(C.Structure):
+    _fields_ = [("batch", C.c_int64), ("row", C.c_int64), ("head", C.c_int64)]
+
+
+class VfAttnShape(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("batch", C.c_int32), ("q_rows", C.c_int32), ("k_rows", C.c_int32),
+                ("q_heads", C.c_int32), ("kv_heads", C.c_int32), ("d_head", C.c_int32), ("scale", C.c_float),
+                ("q", VfAttnLayout), ("k", VfAttnLayout), ("v", VfAttnLayout), ("o", VfAttnLayout),
+                ("d_o", VfAttnLayout), ("dq", VfAttnLayout), ("dk", VfAttnLayout), ("dv", VfAttnLayout)]
+
+
 _SIGNATURES = {
     "vf_partition": (C.c_int, [C.POINTER(C.c_int32), C.c_int32, C.c_int32, C.POINTER(C.c_int32),
                                C.POINTER(C.c_float)]),
@@ -92,6 +111,23 @@ _SIGNATURES = {
     "vf_state_bytes": (C.c_int64, [C.c_void_p]),
     "vf_state_export": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64]),
     "vf_state_import": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64]),
+    "vf_rope_make": (C.c_int, [C.c_int32, C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_int64, C.c_double,
+                               C.c_double, C.c_double, C.POINTER(VfRopePlan)]),
+    "vf_rope": (C.c_int, [C.c_int32, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_int64,
+                          C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_int64, C.POINTER(VfRopePlan), C.c_int32,
+                          C.c_void_p]),
+    "vf_qk_norm_rope": (C.c_int, [C.c_int32, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_int64,
+                                  C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_float,
+                                  C.c_void_p, C.c_int64, C.c_int64, C.POINTER(VfRopePlan), C.c_void_p]),
+    "vf_qk_norm_rope_backward": (C.c_int, [C.c_int32, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_int64,
+                                           C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32,
+                                           C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_int64, C.c_int64,
+                                           C.POINTER(VfRopePlan), C.c_void_p, C.c_void_p, C.c_float, C.c_int32,
+                                           C.c_void_p, C.c_int64, C.c_void_p]),
+    "vf_qk_norm_rope_workspace": (C.c_int64, [C.c_int64, C.c_int32, C.c_int32, C.c_int32]),
+    "vf_attention": (C.c_int, [C.POINTER(VfAttnShape)] + [C.c_void_p] * 9 + [C.c_int64, C.c_void_p]),
+    "vf_attention_backward": (C.c_int, [C.POINTER(VfAttnShape)] + [C.c_void_p] * 13 + [C.c_int64, C.c_void_p]),
+    "vf_attention_workspace": (C.c_int64, [C.POINTER(VfAttnShape), C.c_int32]),
     "vf_solve_split": (C.c_int, [C.POINTER(VfDeviceProfile), C.c_int32, C.c_int32, C.c_double,
                                  C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.POINTER(C.c_double)]),
 }
@@ -193,6 +229,192 @@ def vf_gemm_noalloc(A, B, Cout, M: int, N: int, K: int, alpha: float = 1.0, accu
     assert A.stride(-1) == 1 and B.stride(-1) == 1 and Cout.is_contiguous()
     return lib().vf_gemm_noalloc(_ptr(A), A.stride(0), _ptr(B), B.stride(0), _ptr(Cout), M, N, K,
                                  float(alpha), int(bool(accumulate)), int(nsplit), _stream_handle(stream))
+
+
+# ---- operators between an attention block's projections ------------------------------------------------
+
+
+def _refuse(where: str, why: str):
+    raise VfError(VF_EINVAL, where, why)
+
+
+def _operands(where: str, dtype, *tensors):
+    """All tensors (None: not given) on the current device, floating ones of `dtype` with contiguous heads."""
+    import torch
+    dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    for t in tensors:
+        if t is None:
+            continue
+        if t.device.type != "cuda" or t.device.index != dev:
+            _refuse(where, f"a tensor is on {t.device}, not on the current device")
+        if dtype is not None and t.dtype != dtype:
+            _refuse(where, f"tensors of {t.dtype} and {dtype}")
+        if dtype is not None and t.stride(-1) != 1 and t.shape[-1] > 1:
+            _refuse(where, "the elements of a head are not contiguous")
+
+
+def _dense(where: str, t, shape, dtype):
+    """A contiguous side tensor (positions, weights, lengths, statistics) or None."""
+    if t is None:
+        return None
+    _operands(where, None, t)
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        _refuse(where, f"expected a contiguous {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _float_code(where: str, t) -> int:
+    import torch
+    if t.dtype == torch.bfloat16:
+        return VF_BF16
+    if t.dtype == torch.float32:
+        return VF_F32
+    _refuse(where, f"tensors of {t.dtype}")
+
+
+def vf_rope_make(layout: int, rot_dim: int, base: float = 10000.0, scaling: int = VF_ROPE_PLAIN, factor: float = 1.0,
+                 trained_len: int = 0, beta_fast: float = 32.0, beta_slow: float = 1.0, scale: float = 1.0) -> VfRopePlan:
+    """The plan of a position rotation (host only, plain data): kept and given to every call."""
+    plan = VfRopePlan()
+    _check(lib().vf_rope_make(int(layout), int(rot_dim), float(base), int(scaling), float(factor), int(trained_len),
+                              float(beta_fast), float(beta_slow), float(scale), C.byref(plan)), "vf_rope_make")
+    return plan
+
+
+def vf_rope(x, y, plan: VfRopePlan, positions=None, first: int = 0, seq_len: int = 0, inverse: bool = False, stream=None):
+    """y = x with the heads turned by their rows' positions (inverse: the backward pass).  x, y: [rows, heads, d_head]
+    of any row and head strides; y may be x.  positions: int32 [rows], or None: first + row (% seq_len)."""
+    import torch
+    where = "vf_rope"
+    _operands(where, x.dtype, x, y)
+    if x.dim() != 3 or y.shape != x.shape:
+        _refuse(where, "x and y are [rows, heads, d_head]")
+    rows, heads, dh = x.shape
+    xs, ys = x.stride(), y.stride()
+    _check(lib().vf_rope(_float_code(where, x), x.data_ptr(), xs[0], xs[1], y.data_ptr(), ys[0], ys[1], rows, heads, dh,
+                         _dense(where, positions, (rows,), torch.int32), first, seq_len, C.byref(plan), int(bool(inverse)),
+                         _stream_handle(stream)), where)
+
+
+def vf_qk_norm_rope(x, y, q_heads: int, gamma_q=None, gamma_k=None, eps: float = 1e-6, plan: Optional[VfRopePlan] = None,
+                    positions=None, first: int = 0, seq_len: int = 0, stream=None):
+    """RMS norm of every head (weights gamma_q for the first q_heads heads, gamma_k for the others; None: ones) and, with a
+    plan, the rotation.  x, y: [rows, heads, d_head]; y may be x."""
+    import torch
+    where = "vf_qk_norm_rope"
+    _operands(where, x.dtype, x, y)
+    if x.dim() != 3 or y.shape != x.shape:
+        _refuse(where, "x and y are [rows, heads, d_head]")
+    rows, heads, dh = x.shape
+    xs, ys = x.stride(), y.stride()
+    _check(lib().vf_qk_norm_rope(_float_code(where, x), x.data_ptr(), xs[0], xs[1], y.data_ptr(), ys[0], ys[1], rows,
+                                 q_heads, heads - q_heads, dh, _dense(where, gamma_q, (dh,), torch.float32),
+                                 _dense(where, gamma_k, (dh,), torch.float32), eps,
+                                 _dense(where, positions, (rows,), torch.int32), first, seq_len,
+                                 C.byref(plan) if plan is not None else None, _stream_handle(stream)), where)
+
+
+def vf_qk_norm_rope_workspace(rows: int, q_heads: int, k_heads: int, d_head: int) -> int:
+    """Bytes of workspace vf_qk_norm_rope_backward needs for gradients of the weights."""
+    n = int(lib().vf_qk_norm_rope_workspace(rows, q_heads, k_heads, d_head))
+    if n < 0:
+        _check(n, "vf_qk_norm_rope_workspace")
+    return n
+
+
+def vf_qk_norm_rope_backward(x, dy, dx, q_heads: int, gamma_q=None, gamma_k=None, dgamma_q=None, dgamma_k=None, workspace=None,
+                             eps: float = 1e-6, plan: Optional[VfRopePlan] = None, positions=None, first: int = 0,
+                             seq_len: int = 0, alpha: float = 1.0, accumulate: bool = False, stream=None):
+    """dx from dy (dx may be x or dy); dgamma = alpha * its sum over rows and heads (+ dgamma if accumulate)."""
+    import torch
+    where = "vf_qk_norm_rope_backward"
+    _operands(where, x.dtype, x, dy, dx)
+    _operands(where, None, workspace)
+    if x.dim() != 3 or dy.shape != x.shape or dx.shape != x.shape:
+        _refuse(where, "x, dy and dx are [rows, heads, d_head]")
+    rows, heads, dh = x.shape
+    xs, gs, ds = x.stride(), dy.stride(), dx.stride()
+    f32 = torch.float32
+    _check(lib().vf_qk_norm_rope_backward(
+        _float_code(where, x), x.data_ptr(), xs[0], xs[1], dy.data_ptr(), gs[0], gs[1], dx.data_ptr(), ds[0], ds[1], rows,
+        q_heads, heads - q_heads, dh, _dense(where, gamma_q, (dh,), f32), _dense(where, gamma_k, (dh,), f32), eps,
+        _dense(where, positions, (rows,), torch.int32), first, seq_len, C.byref(plan) if plan is not None else None,
+        _dense(where, dgamma_q, (dh,), f32), _dense(where, dgamma_k, (dh,), f32), alpha, int(bool(accumulate)),
+        workspace.data_ptr() if workspace is not None else None, workspace.numel() * workspace.element_size() if workspace is not None else 0,
+        _stream_handle(stream)), where)
+
+
+def _attn_layout(t) -> VfAttnLayout:
+    s = t.stride()
+    return VfAttnLayout(s[0], s[1], s[2])
+
+
+def _attn_shape(where: str, q, k, v, scale) -> VfAttnShape:
+    if q.dim() != 4 or k.dim() != 4 or v.shape != k.shape:
+        _refuse(where, "q is [batch, q_rows, q_heads, d_head], k and v are [batch, k_rows, kv_heads, d_head]")
+    B, Tq, Hq, dh = q.shape
+    if k.shape[0] != B or k.shape[3] != dh:
+        _refuse(where, "q, k and v differ in batch or head size")
+    return VfAttnShape(_float_code(where, q), B, Tq, k.shape[1], Hq, k.shape[2], dh, dh ** -0.5 if scale is None else scale,
+                       _attn_layout(q), _attn_layout(k), _attn_layout(v))
+
+
+def _attn_masks(where: str, q, k, q_len, k_len, key_mask):
+    import torch
+    B = q.shape[0]
+    if key_mask is not None and key_mask.dtype == torch.bool:
+        key_mask = key_mask.view(torch.uint8)
+    return (_dense(where, q_len, (B,), torch.int32), _dense(where, k_len, (B,), torch.int32),
+            _dense(where, key_mask, (B, k.shape[1]), torch.uint8))
+
+
+def _space(workspace):
+    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+
+
+def vf_attention_workspace(q, k, v, backward: bool = False) -> int:
+    """Bytes of workspace the call over tensors of these shapes needs."""
+    s = _attn_shape("vf_attention_workspace", q, k, v, None)
+    n = int(lib().vf_attention_workspace(C.byref(s), int(bool(backward))))
+    if n < 0:
+        _check(n, "vf_attention_workspace")
+    return n
+
+
+def vf_attention(q, k, v, o, lse=None, q_len=None, k_len=None, key_mask=None, scale=None, workspace=None, stream=None):
+    """o = softmax(scale q k^T) v over the visible keys.  q, o: [batch, q_rows, q_heads, d_head]; k, v: [batch, k_rows,
+    kv_heads, d_head]; lse: fp32 [batch, q_heads, q_rows] for the backward pass; q_len, k_len: int32 [batch]; key_mask:
+    uint8 or bool [batch, k_rows]; scale: 1 / sqrt(d_head) if None."""
+    import torch
+    where = "vf_attention"
+    _operands(where, q.dtype, q, k, v, o)
+    _operands(where, None, workspace)
+    s = _attn_shape(where, q, k, v, scale)
+    if o.shape != q.shape:
+        _refuse(where, "o has the shape of q")
+    s.o = _attn_layout(o)
+    ws, size = _space(workspace)
+    _check(lib().vf_attention(C.byref(s), q.data_ptr(), k.data_ptr(), v.data_ptr(), *_attn_masks(where, q, k, q_len, k_len, key_mask),
+                              o.data_ptr(), _dense(where, lse, (s.batch, s.q_heads, s.q_rows), torch.float32), ws, size,
+                              _stream_handle(stream)), where)
+
+
+def vf_attention_backward(q, k, v, o, lse, d_o, dq, dk, dv, q_len=None, k_len=None, key_mask=None, scale=None, workspace=None,
+                          stream=None):
+    """Gradients dq, dk, dv from d_o; o and lse as vf_attention wrote them, the same lengths, mask and scale."""
+    import torch
+    where = "vf_attention_backward"
+    _operands(where, q.dtype, q, k, v, o, d_o, dq, dk, dv)
+    _operands(where, None, workspace)
+    s = _attn_shape(where, q, k, v, scale)
+    if o.shape != q.shape or d_o.shape != q.shape or dq.shape != q.shape or dk.shape != k.shape or dv.shape != k.shape:
+        _refuse(where, "o, d_o and dq have the shape of q, dk and dv that of k")
+    s.o, s.d_o, s.dq, s.dk, s.dv = _attn_layout(o), _attn_layout(d_o), _attn_layout(dq), _attn_layout(dk), _attn_layout(dv)
+    ws, size = _space(workspace)
+    _check(lib().vf_attention_backward(C.byref(s), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                       *_attn_masks(where, q, k, q_len, k_len, key_mask), o.data_ptr(),
+                                       _dense(where, lse, (s.batch, s.q_heads, s.q_rows), torch.float32), d_o.data_ptr(),
+                                       dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ws, size, _stream_handle(stream)), where)
 
 
 def parse_state(payload: np.ndarray) -> dict:

@@ -543,4 +543,47 @@ int launch_softmax_rows_bwd(float* dP, const void* P, int p_is_bf16, int64_t row
 // out[r,c] = sum of slabs
 int launch_reduce_slabs(const float* in, int nsplit, int64_t slab, int64_t n, float* out, hipStream_t s);
 
+// ---------------------------------------------------------------------------------------
+// operators between an attention block's projections (k_rope.hip, k_xattn.hip)
+// ---------------------------------------------------------------------------------------
+// Rotation / norm of heads: tensors [rows, heads, dh], strides in elements.
+struct RopeJob {
+  const void* x; int64_t x_row, x_head;
+  void* y; int64_t y_row, y_head;                        // backward: dx
+  const void* dy; int64_t dy_row, dy_head;               // backward only
+  int64_t rows;
+  int heads, q_heads, dh;                                // heads from q_heads on take gamma_k
+  const float *gamma_q, *gamma_k;
+  float eps;
+  const int32_t* positions;
+  int64_t first, seq_len;
+  int layout, rot;                                       // rot = 0: nothing turns
+  float scale, sign;
+  float* partial;                                        // backward: partial sums of dgamma, or null
+  int tile, take, q_blocks, lane_bits;                   // set by the launcher
+};
+int launch_rope(int dtype, RopeJob j, const vf_rope_plan* plan, bool norm, hipStream_t st);
+int64_t rope_partial_floats(int64_t rows, int q_heads, int k_heads, int dh);
+int launch_norm_bwd(int dtype, RopeJob j, const vf_rope_plan* plan, float* dgamma_q, float* dgamma_k, float alpha,
+                    int accumulate, hipStream_t st);
+
+// Attention to keys of another length.  The query heads that share a key head are rows of one problem:
+// row r of (batch b, key head hk) is query r / group of head hk * group + r % group.
+struct AttnJob {
+  vf_attn_shape s;
+  int group;                                             // query heads per key head
+  uint32_t group_inv;                                    // floor(r / group) = umulhi(r, group_inv) for every row (group > 1)
+  const void *q, *k, *v;
+  const int32_t *q_len, *k_len;
+  const uint8_t* key_mask;
+  void* o;
+  float* lse;
+  const void* d_o;
+  void *dq, *dk, *dv;
+  float *row_lse, *row_delta;                            // backward: log2-domain lse and rowsum(dO o) of every row, in row order
+};
+int64_t attn_workspace_bytes(const vf_attn_shape& s, bool backward);
+int launch_attn(const AttnJob& j, void* workspace, hipStream_t st);
+int launch_attn_bwd(AttnJob j, void* workspace, hipStream_t st);
+
 }  // namespace vf
