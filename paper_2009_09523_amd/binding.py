@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -125,9 +126,9 @@ _SIGNATURES = {
                                            C.POINTER(VfRopePlan), C.c_void_p, C.c_void_p, C.c_float, C.c_int32,
                                            C.c_void_p, C.c_int64, C.c_void_p]),
     "vf_qk_norm_rope_workspace": (C.c_int64, [C.c_int64, C.c_int32, C.c_int32, C.c_int32]),
-    "vf_attention": (C.c_int, [C.POINTER(VfAttnShape)] + [C.c_void_p] * 9 + [C.c_int64, C.c_void_p]),
-    "vf_attention_backward": (C.c_int, [C.POINTER(VfAttnShape)] + [C.c_void_p] * 13 + [C.c_int64, C.c_void_p]),
-    "vf_attention_workspace": (C.c_int64, [C.POINTER(VfAttnShape), C.c_int32]),
+    "vf_attention": (C.c_int, [C.c_void_p] * 10 + [C.c_int64, C.c_void_p]),
+    "vf_attention_backward": (C.c_int, [C.c_void_p] * 14 + [C.c_int64, C.c_void_p]),
+    "vf_attention_workspace": (C.c_int64, [C.c_void_p, C.c_int32]),
     "vf_solve_split": (C.c_int, [C.POINTER(VfDeviceProfile), C.c_int32, C.c_int32, C.c_double,
                                  C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.POINTER(C.c_double)]),
 }
@@ -234,40 +235,60 @@ def vf_gemm_noalloc(A, B, Cout, M: int, N: int, K: int, alpha: float = 1.0, accu
 # ---- operators between an attention block's projections ------------------------------------------------
 
 
+# These calls are made many times a step on tensors that may be small, so the checks are written to cost little: a call
+# spends 3 to 6 us here and in ctypes beside the 3 to 4 us of a kernel launch.
+
+
 def _refuse(where: str, why: str):
     raise VfError(VF_EINVAL, where, why)
 
 
-def _operands(where: str, dtype, *tensors):
-    """All tensors (None: not given) on the current device, floating ones of `dtype` with contiguous heads."""
+def _device_of(where: str, t) -> int:
+    """The current device, on which the first operand has to be (the others are held against it)."""
     import torch
-    dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
-    for t in tensors:
-        if t is None:
-            continue
-        if t.device.type != "cuda" or t.device.index != dev:
-            _refuse(where, f"a tensor is on {t.device}, not on the current device")
-        if dtype is not None and t.dtype != dtype:
-            _refuse(where, f"tensors of {t.dtype} and {dtype}")
-        if dtype is not None and t.stride(-1) != 1 and t.shape[-1] > 1:
-            _refuse(where, "the elements of a head are not contiguous")
+    dev = t.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
+        _refuse(where, f"a tensor is on {t.device}, not on the current device")
+    return dev
 
 
-def _dense(where: str, t, shape, dtype):
-    """A contiguous side tensor (positions, weights, lengths, statistics) or None."""
+def _operand(where: str, t, like, dev: int):
+    """Strides of a floating operand of `like`'s type with contiguous heads."""
+    if t.get_device() != dev:
+        _refuse(where, f"a tensor is on {t.device}, not on the current device")
+    if t.dtype is not like.dtype:
+        _refuse(where, f"tensors of {t.dtype} and {like.dtype}")
+    s = t.stride()
+    if not s or s[-1] != 1 and t.shape[-1] > 1:
+        _refuse(where, "the elements of a head are not contiguous")
+    return s
+
+
+def _side(where: str, t, dev: int, shape, dtype):
+    """Address of a contiguous side tensor (positions, weights, lengths, statistics) or None."""
     if t is None:
         return None
-    _operands(where, None, t)
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.get_device() != dev:
+        _refuse(where, f"a tensor is on {t.device}, not on the current device")
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         _refuse(where, f"expected a contiguous {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
     return t.data_ptr()
 
 
+def _space(where: str, t, dev: int):
+    """Address and bytes of a workspace (any contiguous tensor) or nothing."""
+    if t is None:
+        return None, 0
+    if t.get_device() != dev or not t.is_contiguous():
+        _refuse(where, "the workspace is not a contiguous tensor on the current device")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
 def _float_code(where: str, t) -> int:
     import torch
-    if t.dtype == torch.bfloat16:
+    if t.dtype is torch.bfloat16:
         return VF_BF16
-    if t.dtype == torch.float32:
+    if t.dtype is torch.float32:
         return VF_F32
     _refuse(where, f"tensors of {t.dtype}")
 
@@ -286,14 +307,16 @@ def vf_rope(x, y, plan: VfRopePlan, positions=None, first: int = 0, seq_len: int
     of any row and head strides; y may be x.  positions: int32 [rows], or None: first + row (% seq_len)."""
     import torch
     where = "vf_rope"
-    _operands(where, x.dtype, x, y)
-    if x.dim() != 3 or y.shape != x.shape:
+    dev = _device_of(where, x)
+    xs, ys, shape = _operand(where, x, x, dev), _operand(where, y, x, dev), x.shape
+    if len(shape) != 3 or y.shape != shape:
         _refuse(where, "x and y are [rows, heads, d_head]")
-    rows, heads, dh = x.shape
-    xs, ys = x.stride(), y.stride()
-    _check(lib().vf_rope(_float_code(where, x), x.data_ptr(), xs[0], xs[1], y.data_ptr(), ys[0], ys[1], rows, heads, dh,
-                         _dense(where, positions, (rows,), torch.int32), first, seq_len, C.byref(plan), int(bool(inverse)),
-                         _stream_handle(stream)), where)
+    rows, heads, dh = shape
+    rc = lib().vf_rope(_float_code(where, x), x.data_ptr(), xs[0], xs[1], y.data_ptr(), ys[0], ys[1], rows, heads, dh,
+                       _side(where, positions, dev, (rows,), torch.int32), first, seq_len, C.byref(plan), bool(inverse),
+                       _stream_handle(stream))
+    if rc:
+        _check(rc, where)
 
 
 def vf_qk_norm_rope(x, y, q_heads: int, gamma_q=None, gamma_k=None, eps: float = 1e-6, plan: Optional[VfRopePlan] = None,
@@ -302,16 +325,18 @@ def vf_qk_norm_rope(x, y, q_heads: int, gamma_q=None, gamma_k=None, eps: float =
     plan, the rotation.  x, y: [rows, heads, d_head]; y may be x."""
     import torch
     where = "vf_qk_norm_rope"
-    _operands(where, x.dtype, x, y)
-    if x.dim() != 3 or y.shape != x.shape:
+    dev = _device_of(where, x)
+    xs, ys, shape = _operand(where, x, x, dev), _operand(where, y, x, dev), x.shape
+    if len(shape) != 3 or y.shape != shape:
         _refuse(where, "x and y are [rows, heads, d_head]")
-    rows, heads, dh = x.shape
-    xs, ys = x.stride(), y.stride()
-    _check(lib().vf_qk_norm_rope(_float_code(where, x), x.data_ptr(), xs[0], xs[1], y.data_ptr(), ys[0], ys[1], rows,
-                                 q_heads, heads - q_heads, dh, _dense(where, gamma_q, (dh,), torch.float32),
-                                 _dense(where, gamma_k, (dh,), torch.float32), eps,
-                                 _dense(where, positions, (rows,), torch.int32), first, seq_len,
-                                 C.byref(plan) if plan is not None else None, _stream_handle(stream)), where)
+    rows, heads, dh = shape
+    f32 = torch.float32
+    rc = lib().vf_qk_norm_rope(_float_code(where, x), x.data_ptr(), xs[0], xs[1], y.data_ptr(), ys[0], ys[1], rows, q_heads,
+                               heads - q_heads, dh, _side(where, gamma_q, dev, (dh,), f32), _side(where, gamma_k, dev, (dh,), f32),
+                               eps, _side(where, positions, dev, (rows,), torch.int32), first, seq_len,
+                               C.byref(plan) if plan is not None else None, _stream_handle(stream))
+    if rc:
+        _check(rc, where)
 
 
 def vf_qk_norm_rope_workspace(rows: int, q_heads: int, k_heads: int, d_head: int) -> int:
@@ -328,56 +353,56 @@ def vf_qk_norm_rope_backward(x, dy, dx, q_heads: int, gamma_q=None, gamma_k=None
     """dx from dy (dx may be x or dy); dgamma = alpha * its sum over rows and heads (+ dgamma if accumulate)."""
     import torch
     where = "vf_qk_norm_rope_backward"
-    _operands(where, x.dtype, x, dy, dx)
-    _operands(where, None, workspace)
-    if x.dim() != 3 or dy.shape != x.shape or dx.shape != x.shape:
+    dev = _device_of(where, x)
+    xs, gs, ds, shape = _operand(where, x, x, dev), _operand(where, dy, x, dev), _operand(where, dx, x, dev), x.shape
+    if len(shape) != 3 or dy.shape != shape or dx.shape != shape:
         _refuse(where, "x, dy and dx are [rows, heads, d_head]")
-    rows, heads, dh = x.shape
-    xs, gs, ds = x.stride(), dy.stride(), dx.stride()
-    f32 = torch.float32
-    _check(lib().vf_qk_norm_rope_backward(
+    rows, heads, dh = shape
+    f32, one = torch.float32, (dh,)
+    ws, size = _space(where, workspace, dev)
+    rc = lib().vf_qk_norm_rope_backward(
         _float_code(where, x), x.data_ptr(), xs[0], xs[1], dy.data_ptr(), gs[0], gs[1], dx.data_ptr(), ds[0], ds[1], rows,
-        q_heads, heads - q_heads, dh, _dense(where, gamma_q, (dh,), f32), _dense(where, gamma_k, (dh,), f32), eps,
-        _dense(where, positions, (rows,), torch.int32), first, seq_len, C.byref(plan) if plan is not None else None,
-        _dense(where, dgamma_q, (dh,), f32), _dense(where, dgamma_k, (dh,), f32), alpha, int(bool(accumulate)),
-        workspace.data_ptr() if workspace is not None else None, workspace.numel() * workspace.element_size() if workspace is not None else 0,
-        _stream_handle(stream)), where)
+        q_heads, heads - q_heads, dh, _side(where, gamma_q, dev, one, f32), _side(where, gamma_k, dev, one, f32), eps,
+        _side(where, positions, dev, (rows,), torch.int32), first, seq_len, C.byref(plan) if plan is not None else None,
+        _side(where, dgamma_q, dev, one, f32), _side(where, dgamma_k, dev, one, f32), alpha, bool(accumulate), ws, size,
+        _stream_handle(stream))
+    if rc:
+        _check(rc, where)
 
 
-def _attn_layout(t) -> VfAttnLayout:
-    s = t.stride()
-    return VfAttnLayout(s[0], s[1], s[2])
+_ATTN_SHAPE = struct.Struct("=7if24q")       # vf_attn_shape, field for field
+_ATTN_NONE = (0,) * 12
 
 
-def _attn_shape(where: str, q, k, v, scale) -> VfAttnShape:
-    if q.dim() != 4 or k.dim() != 4 or v.shape != k.shape:
+def _attn_sizes(where: str, q, k, v, scale):
+    """(the fields of vf_attn_shape before the layouts)"""
+    shape, ks = q.shape, k.shape
+    if len(shape) != 4 or len(ks) != 4 or v.shape != ks:
         _refuse(where, "q is [batch, q_rows, q_heads, d_head], k and v are [batch, k_rows, kv_heads, d_head]")
-    B, Tq, Hq, dh = q.shape
-    if k.shape[0] != B or k.shape[3] != dh:
+    B, Tq, Hq, dh = shape
+    if ks[0] != B or ks[3] != dh:
         _refuse(where, "q, k and v differ in batch or head size")
-    return VfAttnShape(_float_code(where, q), B, Tq, k.shape[1], Hq, k.shape[2], dh, dh ** -0.5 if scale is None else scale,
-                       _attn_layout(q), _attn_layout(k), _attn_layout(v))
+    if max(B, Tq, ks[1], Hq, ks[2], dh) > 0x7fffffff:
+        _refuse(where, "a size is beyond 32 bits")
+    return _float_code(where, q), B, Tq, ks[1], Hq, ks[2], dh, dh ** -0.5 if scale is None else scale
 
 
-def _attn_masks(where: str, q, k, q_len, k_len, key_mask):
+def _attn_masks(where: str, dev: int, B: int, Tk: int, q_len, k_len, key_mask):
+    if q_len is None and k_len is None and key_mask is None:
+        return None, None, None
     import torch
-    B = q.shape[0]
-    if key_mask is not None and key_mask.dtype == torch.bool:
+    if key_mask is not None and key_mask.dtype is torch.bool:
         key_mask = key_mask.view(torch.uint8)
-    return (_dense(where, q_len, (B,), torch.int32), _dense(where, k_len, (B,), torch.int32),
-            _dense(where, key_mask, (B, k.shape[1]), torch.uint8))
-
-
-def _space(workspace):
-    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    return (_side(where, q_len, dev, (B,), torch.int32), _side(where, k_len, dev, (B,), torch.int32),
+            _side(where, key_mask, dev, (B, Tk), torch.uint8))
 
 
 def vf_attention_workspace(q, k, v, backward: bool = False) -> int:
     """Bytes of workspace the call over tensors of these shapes needs."""
-    s = _attn_shape("vf_attention_workspace", q, k, v, None)
-    n = int(lib().vf_attention_workspace(C.byref(s), int(bool(backward))))
+    where = "vf_attention_workspace"
+    n = int(lib().vf_attention_workspace(_ATTN_SHAPE.pack(*_attn_sizes(where, q, k, v, 1.0), *_ATTN_NONE, *_ATTN_NONE), bool(backward)))
     if n < 0:
-        _check(n, "vf_attention_workspace")
+        _check(n, where)
     return n
 
 
@@ -387,16 +412,17 @@ def vf_attention(q, k, v, o, lse=None, q_len=None, k_len=None, key_mask=None, sc
     uint8 or bool [batch, k_rows]; scale: 1 / sqrt(d_head) if None."""
     import torch
     where = "vf_attention"
-    _operands(where, q.dtype, q, k, v, o)
-    _operands(where, None, workspace)
-    s = _attn_shape(where, q, k, v, scale)
+    dev = _device_of(where, q)
+    lay = (*_operand(where, q, q, dev)[:3], *_operand(where, k, q, dev)[:3], *_operand(where, v, q, dev)[:3], *_operand(where, o, q, dev)[:3])
+    sizes = _attn_sizes(where, q, k, v, scale)
     if o.shape != q.shape:
         _refuse(where, "o has the shape of q")
-    s.o = _attn_layout(o)
-    ws, size = _space(workspace)
-    _check(lib().vf_attention(C.byref(s), q.data_ptr(), k.data_ptr(), v.data_ptr(), *_attn_masks(where, q, k, q_len, k_len, key_mask),
-                              o.data_ptr(), _dense(where, lse, (s.batch, s.q_heads, s.q_rows), torch.float32), ws, size,
-                              _stream_handle(stream)), where)
+    ws, size = _space(where, workspace, dev)
+    rc = lib().vf_attention(_ATTN_SHAPE.pack(*sizes, *lay, *_ATTN_NONE), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                            *_attn_masks(where, dev, sizes[1], sizes[3], q_len, k_len, key_mask), o.data_ptr(),
+                            _side(where, lse, dev, (sizes[1], sizes[4], sizes[2]), torch.float32), ws, size, _stream_handle(stream))
+    if rc:
+        _check(rc, where)
 
 
 def vf_attention_backward(q, k, v, o, lse, d_o, dq, dk, dv, q_len=None, k_len=None, key_mask=None, scale=None, workspace=None,
@@ -404,17 +430,18 @@ def vf_attention_backward(q, k, v, o, lse, d_o, dq, dk, dv, q_len=None, k_len=No
     """Gradients dq, dk, dv from d_o; o and lse as vf_attention wrote them, the same lengths, mask and scale."""
     import torch
     where = "vf_attention_backward"
-    _operands(where, q.dtype, q, k, v, o, d_o, dq, dk, dv)
-    _operands(where, None, workspace)
-    s = _attn_shape(where, q, k, v, scale)
-    if o.shape != q.shape or d_o.shape != q.shape or dq.shape != q.shape or dk.shape != k.shape or dv.shape != k.shape:
+    dev = _device_of(where, q)
+    lay = [x for t in (q, k, v, o, d_o, dq, dk, dv) for x in _operand(where, t, q, dev)[:3]]
+    sizes = _attn_sizes(where, q, k, v, scale)
+    if not q.shape == o.shape == d_o.shape == dq.shape or not k.shape == dk.shape == dv.shape:
         _refuse(where, "o, d_o and dq have the shape of q, dk and dv that of k")
-    s.o, s.d_o, s.dq, s.dk, s.dv = _attn_layout(o), _attn_layout(d_o), _attn_layout(dq), _attn_layout(dk), _attn_layout(dv)
-    ws, size = _space(workspace)
-    _check(lib().vf_attention_backward(C.byref(s), q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                                       *_attn_masks(where, q, k, q_len, k_len, key_mask), o.data_ptr(),
-                                       _dense(where, lse, (s.batch, s.q_heads, s.q_rows), torch.float32), d_o.data_ptr(),
-                                       dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ws, size, _stream_handle(stream)), where)
+    ws, size = _space(where, workspace, dev)
+    rc = lib().vf_attention_backward(_ATTN_SHAPE.pack(*sizes, *lay), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                     *_attn_masks(where, dev, sizes[1], sizes[3], q_len, k_len, key_mask), o.data_ptr(),
+                                     _side(where, lse, dev, (sizes[1], sizes[4], sizes[2]), torch.float32), d_o.data_ptr(),
+                                     dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ws, size, _stream_handle(stream))
+    if rc:
+        _check(rc, where)
 
 
 def parse_state(payload: np.ndarray) -> dict:

@@ -299,7 +299,9 @@ __global__ __launch_bounds__(NT) void norm_bwd_kernel(RopeJob j, Turns turns) {
   }
 }
 
-// dgamma = alpha (sum of the partials, in order) (+ dgamma).  Workgroup (column block of 64, class).
+// dgamma = alpha (sum of the partials, in order) (+ dgamma).  Workgroup (16 columns, class): 64 groups of 16 threads take
+// every 64th partial, four loads under way at a time, and their sums are added in the order of the groups.  (512 partials of
+// 64 columns: with 16 groups of 64 columns, one load after the other, 9.3 us.)
 struct GammaFinish {
   const float* partial[2];
   int64_t count[2];
@@ -307,21 +309,30 @@ struct GammaFinish {
   float alpha;
   int accumulate, dh;
 };
-constexpr int FIN_GROUPS = 16;
-__global__ __launch_bounds__(64 * FIN_GROUPS) void gamma_finish_kernel(GammaFinish f) {
-  __shared__ float part[FIN_GROUPS][64];
-  const int c = blockIdx.x * 64 + (threadIdx.x & 63), g = threadIdx.x >> 6;
-  const int which = blockIdx.y;
+constexpr int FIN_COLS = 16, FIN_GROUPS = 64;
+__global__ __launch_bounds__(FIN_COLS * FIN_GROUPS) void gamma_finish_kernel(GammaFinish f) {
+  __shared__ float part[FIN_GROUPS][FIN_COLS + 1];
+  const int which = blockIdx.y, t = threadIdx.x % FIN_COLS, g = threadIdx.x / FIN_COLS;
+  const int c = blockIdx.x * FIN_COLS + t;
   if (!f.out[which]) return;
   float v = 0.f;
-  if (c < f.dh)
-    for (int64_t i = g; i < f.count[which]; i += FIN_GROUPS) v += f.partial[which][i * f.dh + c];
-  part[g][threadIdx.x & 63] = v;
+  if (c < f.dh) {
+    const float* p = f.partial[which] + c;
+    const int n = (int)f.count[which];
+    for (int i = g; i < n; i += 4 * FIN_GROUPS) {
+      float x[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) x[u] = i + u * FIN_GROUPS < n ? p[(int64_t)(i + u * FIN_GROUPS) * f.dh] : 0.f;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v += x[u];
+    }
+  }
+  part[g][t] = v;
   __syncthreads();
   if (g == 0 && c < f.dh) {
     float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < FIN_GROUPS; ++i) sum += part[i][threadIdx.x];
+    for (int i = 0; i < FIN_GROUPS; ++i) sum += part[i][t];
     GradOut o{f.out[which], f.alpha, f.accumulate};
     grad_store(o, c, sum);
   }
@@ -426,7 +437,7 @@ int launch_norm_bwd(int dtype, RopeJob j, const vf_rope_plan* plan, float* dgamm
   f.count[1] = (int64_t)grid.x * grid.y - qn;
   f.out[0] = dgamma_q; f.out[1] = dgamma_k;
   f.alpha = alpha; f.accumulate = accumulate; f.dh = j.dh;
-  gamma_finish_kernel<<<dim3((unsigned)((j.dh + 63) / 64), 2), 64 * FIN_GROUPS, 0, st>>>(f);
+  gamma_finish_kernel<<<dim3((unsigned)((j.dh + FIN_COLS - 1) / FIN_COLS), 2), FIN_COLS * FIN_GROUPS, 0, st>>>(f);
   VF_LAUNCH_CHECK();
   return VF_OK;
 }

@@ -13,6 +13,7 @@
 // The query heads that share a key head are rows of one problem (row r = query r / group of head r % group), so the keys
 // are read once for all of them and the gradients of shared keys are summed in registers.
 #include <algorithm>
+#include <atomic>
 
 #include "vf_device.h"
 
@@ -502,10 +503,22 @@ __global__ __launch_bounds__(NT, 1) void xattn_dkv_kernel(AttnJob j, int tiles) 
   store_row<T, DP>(at<T>(j.dv, j.s.dv, p.b, key, p.hk), dv, 1.f, dh, half);
 }
 
+// LDS above 64 KB has to be allowed for a kernel once on every device.
+int allow_lds(const void* kernel, int bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  VF_HIP(hipGetDevice(&dev));
+  const uint64_t bit = 1ull << (dev & 63);
+  if (done.load(std::memory_order_relaxed) & bit) return VF_OK;
+  VF_HIP(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  if (dev < 64) done.fetch_or(bit, std::memory_order_relaxed);
+  return VF_OK;
+}
+
 template <typename T, int DP>
 int launch_fwd(const AttnJob& j, hipStream_t st) {
   constexpr int lds = 4 * Tile<T, DP>::ELEMS * sizeof(T);
-  VF_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&xattn_fwd_kernel<T, DP>), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+  static std::atomic<uint64_t> ready{0};
+  VF_TRY(allow_lds(reinterpret_cast<const void*>(&xattn_fwd_kernel<T, DP>), lds, ready));
   const int tiles = (j.group * j.s.q_rows + 4 * WR - 1) / (4 * WR);
   xattn_fwd_kernel<T, DP><<<j.s.batch * j.s.kv_heads * tiles, NT, lds, st>>>(j, tiles);
   VF_LAUNCH_CHECK();
@@ -515,8 +528,9 @@ int launch_fwd(const AttnJob& j, hipStream_t st) {
 template <typename T, int DP>
 int launch_bwd(const AttnJob& j, hipStream_t st) {
   constexpr int lds = 4 * Tile<T, DP>::ELEMS * sizeof(T), lds_kv = lds + 4 * Elem<T>::TR * sizeof(float);
-  VF_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&xattn_dq_kernel<T, DP>), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
-  VF_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&xattn_dkv_kernel<T, DP>), hipFuncAttributeMaxDynamicSharedMemorySize, lds_kv));
+  static std::atomic<uint64_t> ready_q{0}, ready_kv{0};
+  VF_TRY(allow_lds(reinterpret_cast<const void*>(&xattn_dq_kernel<T, DP>), lds, ready_q));
+  VF_TRY(allow_lds(reinterpret_cast<const void*>(&xattn_dkv_kernel<T, DP>), lds_kv, ready_kv));
   const int heads = j.s.batch * j.s.kv_heads;
   const int qt = (j.group * j.s.q_rows + 4 * WR - 1) / (4 * WR), kt = (j.s.k_rows + 4 * WR - 1) / (4 * WR);
   if (qt) {

@@ -169,6 +169,9 @@ def test_structures_match_the_header():
         body = text[text.index("typedef struct %s {" % name):text.index("} %s;" % name)].split("{", 1)[1]
         names = [re.sub(r"\[.*\]", "", n.strip()) for d in body.split(";") if len(d.split(None, 1)) == 2 for n in d.split(None, 1)[1].split(",")]
         assert names == [f[0] for f in cls._fields_]
+    assert binding._ATTN_SHAPE.size == C.sizeof(binding.VfAttnShape)
+    packed = binding.VfAttnShape.from_buffer_copy(binding._ATTN_SHAPE.pack(*range(7), 0.5, *range(24)))
+    assert packed.d_head == 6 and packed.scale == 0.5 and packed.q.batch == 0 and packed.d_o.row == 13 and packed.dv.head == 23
 
 
 def test_binding_refuses_tensors_that_are_not_on_the_device():
