@@ -151,29 +151,43 @@ __device__ __forceinline__ void clear(f32x16 (&a)[N]) {
     for (int r = 0; r < 16; ++r) a[i][r] = 0.f;
 }
 
-// A tile on its way from memory: chunks of this thread, in registers until the buffer they go to is free.
+// Tiles go from memory straight into LDS (global_load_lds_dwordx4: the lanes of a wavefront deposit 16 bytes each, side by
+// side), so a tile under way costs no registers, and a ring of STAGES buffers keeps STAGES - 1 of them under way.  The order of
+// chunks in LDS is made on the memory side: a lane fetches the chunk that belongs at its place.  Rows that are padding or
+// invisible and chunks behind the head come from a block of zeros: nothing that lies there in memory reaches a product.
+// Loads of a wavefront complete in order, so "all but the newest n" (vmcnt) says when a tile is there.
+__device__ __attribute__((aligned(16))) uint32_t g_zeros[4];
+__device__ uint32_t g_infinity = 0x7f800000u;
+
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(const void __attribute__((address_space(3)))*)p; }
+__device__ __forceinline__ void lds_load16(const void* src, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(src) : "memory");
+}
+__device__ __forceinline__ void lds_load4(const void* src, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(dst), "v"(src) : "memory");
+}
+// all but the newest N loads there, own LDS reads done; then all wavefronts meet
+template <int N>
+__device__ __forceinline__ void wait_and_meet() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
 template <typename T, int DP>
-struct Stage {
-  static constexpr int CE = Elem<T>::CE, CH = DP / CE, N = Elem<T>::TR * CH / NT;
-  static_assert(Elem<T>::TR * CH % NT == 0, "chunks of a tile over the threads");
-  u32x4 w[N];
-  static __device__ __forceinline__ int row(int i) { return (i * NT + (int)threadIdx.x) / CH; }
-  static __device__ __forceinline__ int chunk(int i) { return (i * NT + (int)threadIdx.x) % CH; }
-  // row_ptr(r): first element of tile row r, or null for a row of zeros
-  template <typename F>
-  __device__ __forceinline__ void fetch(F row_ptr, int dh) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const T* p = row_ptr(row(i));
-      w[i] = u32x4{0u, 0u, 0u, 0u};
-      if (p && chunk(i) * CE < dh) w[i] = *reinterpret_cast<const u32x4*>(p + chunk(i) * CE);
-    }
-  }
-  __device__ __forceinline__ void put(T* tile) const {
-#pragma unroll
-    for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4*>(tile + Tile<T, DP>::pos(row(i), chunk(i))) = w[i];
-  }
+struct Ring {
+  static constexpr int CE = Elem<T>::CE, CH = DP / CE, TR = Elem<T>::TR, N = TR * CH / NT;   // N: loads of a wavefront per tile
+  static constexpr int BYTES = TR * DP * (int)sizeof(T);
+  static constexpr int STAGES = BYTES <= 8192 ? 3 : 2;      // 48 KB (64 KB) for pairs of tiles: three (two) workgroups to a compute unit
+  static_assert(TR * CH % NT == 0, "chunks of a tile over the threads");
 };
+
+// What a workgroup does: tile `tile` of the held rows of problem `id`, a part of the streamed side from tile `first` on.
+// Grid (problems, tiles, parts): neighbouring workgroups go to different XCDs, so with a multiple of 8 problems all workgroups
+// that stream the same rows share an L2.  (A contiguous run of the numbers for each XCD: no faster at 2 x 16 problems of 4096 x
+// 8192 x 128, and three integer divisions a workgroup cost 3 us of 12 where it has two tiles.)
+struct Work { int id, tile, part, first; };
+__device__ __forceinline__ Work work_of(const AttnSplit& sp) {
+  return {(int)blockIdx.x, (int)blockIdx.y, (int)blockIdx.z, (int)blockIdx.z * sp.per};
+}
 
 // One (batch, key head) problem.
 struct Problem {
@@ -186,8 +200,8 @@ __device__ __forceinline__ Problem problem_of(const AttnJob& j, int id) {
   p.b = id / j.s.kv_heads;
   p.hk = id - p.b * j.s.kv_heads;
   p.rows = j.group * j.s.q_rows;
-  p.q_len = j.q_len ? min(max(j.q_len[p.b], 0), j.s.q_rows) : j.s.q_rows;
-  p.keys = j.k_len ? min(max(j.k_len[p.b], 0), j.s.k_rows) : j.s.k_rows;
+  p.q_len = j.q_len ? __builtin_amdgcn_readfirstlane(min(max(j.q_len[p.b], 0), j.s.q_rows)) : j.s.q_rows;
+  p.keys = j.k_len ? __builtin_amdgcn_readfirstlane(min(max(j.k_len[p.b], 0), j.s.k_rows)) : j.s.k_rows;
   return p;
 }
 // query and head (among the group's) of row r
@@ -202,12 +216,86 @@ __device__ __forceinline__ T* at(const void* base, const vf_attn_layout& l, int 
   return const_cast<T*>(static_cast<const T*>(base)) + (int64_t)b * l.batch + (int64_t)row * l.row + (int64_t)head * l.head;
 }
 
-// Which of the keys k0 .. k0 + 63 are visible, one bit each (the same in every lane of the wavefront).
-__device__ __forceinline__ uint64_t visible(const AttnJob& j, const Problem& p, int k0, int lane) {
-  const int k = k0 + lane;
-  bool on = k < p.keys;
-  if (j.key_mask && on) on = j.key_mask[(int64_t)p.b * j.s.k_rows + k] != 0;
-  return __ballot(on);
+// This thread's chunks of one streamed tensor: where they lie for the tile that is loaded next.
+template <typename T, int DP>
+struct Source {
+  static constexpr int N = Ring<T, DP>::N, CH = Ring<T, DP>::CH, CE = Ring<T, DP>::CE, TR = Ring<T, DP>::TR;
+  const char* p[N];
+  int g[N];                     // head among the group's (rows of several heads; else 0)
+  // base: head 0 of row 0; rows r0, r0 + 1, ... are head r % group of row r / group
+  __device__ __forceinline__ void init(const AttnJob& j, const T* base, const vf_attn_layout& l, int r0, bool grouped) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int r = (i * NT + (int)threadIdx.x) / CH;
+      const RowOf ro = grouped ? row_of(j, r0 + r) : RowOf{r0 + r, 0};
+      const int c = Tile<T, DP>::pos(r, (i * NT + (int)threadIdx.x) % CH) - r * DP;   // (the exchange of places undoes itself)
+      p[i] = reinterpret_cast<const char*>(base + (int64_t)ro.t * l.row + (int64_t)ro.g * l.head + c);
+      g[i] = ro.g;
+    }
+  }
+  // bit i: chunk i lies within the head
+  static __device__ __forceinline__ uint32_t head_bits(int dh) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int r = (i * NT + (int)threadIdx.x) / CH;
+      if (Tile<T, DP>::pos(r, (i * NT + (int)threadIdx.x) % CH) - r * DP < dh) m |= 1u << i;
+    }
+    return m;
+  }
+  // rows: bit r: row r of the tile is wanted; tile: LDS address of the tile's buffer for this wavefront
+  __device__ __forceinline__ void issue(uint64_t rows, uint32_t head, bool whole, const char* zeros, uint32_t tile) const {
+    const uint64_t mine = rows >> (threadIdx.x / CH);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const char* src = p[i];
+      if (!whole) src = ((mine >> (i * (NT / CH))) & (head >> i) & 1) ? p[i] : zeros;
+      lds_load16(src, tile + i * (NT * 16));
+    }
+  }
+  __device__ __forceinline__ void advance(int64_t step) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) p[i] += step;
+  }
+  // rows of several heads: step for TR / group rows and TR % group heads, and one more row where the heads run over
+  __device__ __forceinline__ void advance(int64_t step, int64_t over, int heads, int group) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      g[i] += heads;
+      const bool wrap = g[i] >= group;
+      p[i] += step + (wrap ? over : 0);
+      if (wrap) g[i] -= group;
+    }
+  }
+};
+
+__device__ __forceinline__ uint64_t first_bits(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; }
+// An address in scalar registers that is not taken again in the loops.
+__device__ __forceinline__ const char* zeros_address() {
+  const char* z = reinterpret_cast<const char*>(g_zeros);
+  asm volatile("" : "+s"(z));
+  return z;
+}
+
+// Which of the keys k0 .. k0 + 63 (k0 a multiple of 32) are visible, one bit each.  A mask comes as such bits (mask_bits_kernel),
+// read by scalar loads, which do not stand in the queue of the tiles' loads.
+__device__ __forceinline__ uint64_t visible(const AttnJob& j, const Problem& p, int k0) {
+  const int n = p.keys - k0;
+  uint64_t bits = first_bits(n);
+  if (j.bits && n > 0) {
+    const __attribute__((address_space(4))) uint64_t* w = (const __attribute__((address_space(4))) uint64_t*)(j.bits + (int64_t)p.b * j.words + (k0 >> 6));
+    bits &= w[0] >> (k0 & 32);
+  }
+  return bits;
+}
+// bits[b][w], bit i: key 64 w + i of the mask is visible.
+__global__ __launch_bounds__(NT) void mask_bits_kernel(const uint8_t* __restrict__ mask, int keys, int words, int64_t n, uint64_t* __restrict__ bits) {
+  const int64_t w = (int64_t)blockIdx.x * (NT / 64) + (threadIdx.x >> 6);
+  if (w >= n) return;
+  const int64_t b = w / words;
+  const int k = (int)(w - b * words) * 64 + (threadIdx.x & 63);
+  const uint64_t on = __ballot(k < keys && mask[b * keys + k] != 0);
+  if ((threadIdx.x & 63) == 0) bits[w] = on;
 }
 
 // max / sum over the two lanes of a column
@@ -234,13 +322,16 @@ __device__ __forceinline__ void store_row(T* row, const f32x16 (&acc)[DP / 32], 
 
 // ---- forward ------------------------------------------------------------------------------------
 template <typename T, int DP>
-__global__ __launch_bounds__(NT, 2) void xattn_fwd_kernel(AttnJob j, int tiles) {
-  constexpr int TR = Elem<T>::TR, KB = TR / 32, ELEMS = Tile<T, DP>::ELEMS;
+__global__ __launch_bounds__(NT, 2) void xattn_fwd_kernel(AttnJob j, AttnSplit sp) {
+  constexpr int TR = Elem<T>::TR, KB = TR / 32, ELEMS = Tile<T, DP>::ELEMS, STAGES = Ring<T, DP>::STAGES, BYTES = Ring<T, DP>::BYTES;
+  constexpr uint64_t ALL = TR == 64 ? ~0ull : (1ull << TR) - 1;
   extern __shared__ __attribute__((aligned(16))) char xattn_lds[];
-  T* lds = reinterpret_cast<T*>(xattn_lds);                 // [2][k, v][ELEMS]
+  T* lds = reinterpret_cast<T*>(xattn_lds);                 // [STAGES][k, v][ELEMS]
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
-  const Problem p = problem_of(j, blockIdx.x / tiles);
-  const int r = (blockIdx.x % tiles) * (4 * WR) + wave * WR + (lane & 31);
+  const Work w = work_of(sp);
+  const Problem p = problem_of(j, w.id);
+  const int r = w.tile * (4 * WR) + wave * WR + (lane & 31);
+  const int kbeg = w.first * TR, kend = min(p.keys, kbeg + sp.per * TR);
   const bool mine = r < p.rows;
   const RowOf ro = row_of(j, mine ? r : 0);
   const int head = p.hk * j.group + ro.g;
@@ -254,33 +345,37 @@ __global__ __launch_bounds__(NT, 2) void xattn_fwd_kernel(AttnJob j, int tiles) 
   clear(o);
   float m = -INFINITY, l = 0.f;
 
-  const T* kbase = at<const T>(j.k, j.s.k, p.b, 0, p.hk);
-  const T* vbase = at<const T>(j.v, j.s.v, p.b, 0, p.hk);
-  Stage<T, DP> ks, vs;
-  auto fetch = [&](int k0, uint64_t vis) {
-    ks.fetch([&](int t) { return (vis >> t) & 1 ? kbase + (int64_t)(k0 + t) * j.s.k.row : nullptr; }, dh);
-    vs.fetch([&](int t) { return (vis >> t) & 1 ? vbase + (int64_t)(k0 + t) * j.s.v.row : nullptr; }, dh);
+  const uint32_t lds0 = lds_address(lds) + __builtin_amdgcn_readfirstlane(wave) * 1024;
+  const char* const zeros = zeros_address();
+  const uint32_t in_head = Source<T, DP>::head_bits(dh);
+  const int64_t kstep = TR * j.s.k.row * (int64_t)sizeof(T), vstep = TR * j.s.v.row * (int64_t)sizeof(T);
+  Source<T, DP> ks, vs;
+  ks.init(j, at<const T>(j.k, j.s.k, p.b, 0, p.hk), j.s.k, kbeg, false);
+  vs.init(j, at<const T>(j.v, j.s.v, p.b, 0, p.hk), j.s.v, kbeg, false);
+  auto issue = [&](int k0, int buf) {                       // (behind the last tile: zeros, so that every tile counts alike)
+    const uint64_t vis = k0 < kend ? visible(j, p, k0) : 0;
+    const bool whole = dh == DP && (vis & ALL) == ALL;
+    ks.issue(vis, in_head, whole, zeros, lds0 + buf * 2 * BYTES);
+    vs.issue(vis, in_head, whole, zeros, lds0 + buf * 2 * BYTES + BYTES);
+    ks.advance(kstep);
+    vs.advance(vstep);
   };
-  uint64_t vis = p.keys > 0 ? visible(j, p, 0, lane) : 0;
-  if (p.keys > 0) fetch(0, vis);
+  if (kbeg < kend) {
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) issue(kbeg + i * TR, i);
+  }
   int buf = 0;
-  for (int k0 = 0; k0 < p.keys; k0 += TR, buf ^= 1) {
-    T* kt = lds + buf * 2 * ELEMS;
-    T* vt = kt + ELEMS;
-    ks.put(kt);
-    vs.put(vt);
-    const uint64_t now = vis;
-    if (k0 + TR < p.keys) {
-      vis = visible(j, p, k0 + TR, lane);
-      fetch(k0 + TR, vis);
-    }
-    __syncthreads();                                        // (two buffers: the next iteration writes the other one)
+  for (int k0 = kbeg; k0 < kend; k0 += TR, buf = (buf + 1) % STAGES) {
+    const T* kt = lds + buf * 2 * ELEMS;
+    const T* vt = kt + ELEMS;
+    wait_and_meet<(STAGES - 2) * 2 * Ring<T, DP>::N>();     // this tile is there, and nobody reads the one before it
+    issue(k0 + (STAGES - 1) * TR, (buf + STAGES - 1) % STAGES);
+    const uint64_t now = visible(j, p, k0);
     f32x16 s[KB];
     clear(s);
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) dot_rows<T, DP>(s[kb], kt, 32 * kb, q, lane);
-    const uint64_t all = TR == 64 ? ~0ull : 0xffffffffull;
-    if ((now & all) != all) {
+    if ((now & ALL) != ALL) {
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
         const uint32_t bits = (uint32_t)(now >> (32 * kb)) >> (4 * half);
@@ -325,8 +420,16 @@ __global__ __launch_bounds__(NT, 2) void xattn_fwd_kernel(AttnJob j, int tiles) 
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) dot_cols<T, DP>(o, vt, 32 * kb, s[kb], lane);
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // no load may find its LDS given away
   if (!mine) return;
   l = pair_sum(l);
+  if (sp.parts > 1) {                                       // a part: unnormalised, with its maximum and sum
+    const int64_t row = ((int64_t)w.part * j.s.batch * j.s.kv_heads + w.id) * p.rows + r;
+    if (!live) l = 0.f;
+    if (half == 0) *reinterpret_cast<float2*>(sp.stats + 2 * row) = make_float2(m, l);
+    if (l != 0.f) store_row<float, DP>(sp.out[0] + row * dh, o, 1.f, dh, half);
+    return;
+  }
   const bool any = live && l != 0.f;                        // (a NaN goes on)
   store_row<T, DP>(at<T>(j.o, j.s.o, p.b, ro.t, head), o, any ? 1.f / l : 0.f, dh, half);
   if (j.lse && half == 0)
@@ -335,14 +438,16 @@ __global__ __launch_bounds__(NT, 2) void xattn_fwd_kernel(AttnJob j, int tiles) 
 
 // ---- backward: dq, and lse / rowsum(dO o) of every row for the kernel behind it ---------------------
 template <typename T, int DP>
-__global__ __launch_bounds__(NT, 1) void xattn_dq_kernel(AttnJob j, int tiles) {
-  constexpr int TR = Elem<T>::TR, KB = TR / 32, ELEMS = Tile<T, DP>::ELEMS;
+__global__ __launch_bounds__(NT, DP <= 64 ? 2 : 1) void xattn_dq_kernel(AttnJob j, AttnSplit sp) {
+  constexpr int TR = Elem<T>::TR, KB = TR / 32, ELEMS = Tile<T, DP>::ELEMS, STAGES = Ring<T, DP>::STAGES, BYTES = Ring<T, DP>::BYTES;
+  constexpr uint64_t ALL = TR == 64 ? ~0ull : (1ull << TR) - 1;
   extern __shared__ __attribute__((aligned(16))) char xattn_lds[];
   T* lds = reinterpret_cast<T*>(xattn_lds);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
-  const int id = blockIdx.x / tiles;
-  const Problem p = problem_of(j, id);
-  const int r = (blockIdx.x % tiles) * (4 * WR) + wave * WR + (lane & 31);
+  const Work w = work_of(sp);
+  const Problem p = problem_of(j, w.id);
+  const int r = w.tile * (4 * WR) + wave * WR + (lane & 31);
+  const int kbeg = w.first * TR, kend = min(p.keys, kbeg + sp.per * TR);
   const bool mine = r < p.rows;
   const RowOf ro = row_of(j, mine ? r : 0);
   const int head = p.hk * j.group + ro.g;
@@ -372,34 +477,36 @@ __global__ __launch_bounds__(NT, 1) void xattn_dq_kernel(AttnJob j, int tiles) {
       }
     delta = pair_sum(delta);
   }
-  if (mine && half == 0) {
-    j.row_lse[(int64_t)id * p.rows + r] = lse;
-    j.row_delta[(int64_t)id * p.rows + r] = delta;
-  }
   f32x16 dq[DP / 32];
   clear(dq);
+  float rest = 0.f;                                         // sum of dz: 0 with the exact rowsum, here the error of o's rounding
 
-  const T* kbase = at<const T>(j.k, j.s.k, p.b, 0, p.hk);
-  const T* vbase = at<const T>(j.v, j.s.v, p.b, 0, p.hk);
-  Stage<T, DP> ks, vs;
-  auto fetch = [&](int k0, uint64_t vis) {
-    ks.fetch([&](int t) { return (vis >> t) & 1 ? kbase + (int64_t)(k0 + t) * j.s.k.row : nullptr; }, dh);
-    vs.fetch([&](int t) { return (vis >> t) & 1 ? vbase + (int64_t)(k0 + t) * j.s.v.row : nullptr; }, dh);
+  const uint32_t lds0 = lds_address(lds) + __builtin_amdgcn_readfirstlane(wave) * 1024;
+  const char* const zeros = zeros_address();
+  const uint32_t in_head = Source<T, DP>::head_bits(dh);
+  const int64_t kstep = TR * j.s.k.row * (int64_t)sizeof(T), vstep = TR * j.s.v.row * (int64_t)sizeof(T);
+  Source<T, DP> ks, vs;
+  ks.init(j, at<const T>(j.k, j.s.k, p.b, 0, p.hk), j.s.k, kbeg, false);
+  vs.init(j, at<const T>(j.v, j.s.v, p.b, 0, p.hk), j.s.v, kbeg, false);
+  auto issue = [&](int k0, int buf) {                       // (behind the last tile: zeros, so that every tile counts alike)
+    const uint64_t vis = k0 < kend ? visible(j, p, k0) : 0;
+    const bool whole = dh == DP && (vis & ALL) == ALL;
+    ks.issue(vis, in_head, whole, zeros, lds0 + buf * 2 * BYTES);
+    vs.issue(vis, in_head, whole, zeros, lds0 + buf * 2 * BYTES + BYTES);
+    ks.advance(kstep);
+    vs.advance(vstep);
   };
-  uint64_t vis = p.keys > 0 ? visible(j, p, 0, lane) : 0;
-  if (p.keys > 0) fetch(0, vis);
+  if (kbeg < kend) {
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) issue(kbeg + i * TR, i);
+  }
   int buf = 0;
-  for (int k0 = 0; k0 < p.keys; k0 += TR, buf ^= 1) {
-    T* kt = lds + buf * 2 * ELEMS;
-    T* vt = kt + ELEMS;
-    ks.put(kt);
-    vs.put(vt);
-    const uint64_t now = vis;
-    if (k0 + TR < p.keys) {
-      vis = visible(j, p, k0 + TR, lane);
-      fetch(k0 + TR, vis);
-    }
-    __syncthreads();
+  for (int k0 = kbeg; k0 < kend; k0 += TR, buf = (buf + 1) % STAGES) {
+    const T* kt = lds + buf * 2 * ELEMS;
+    const T* vt = kt + ELEMS;
+    wait_and_meet<(STAGES - 2) * 2 * Ring<T, DP>::N>();     // this tile is there, and nobody reads the one before it
+    issue(k0 + (STAGES - 1) * TR, (buf + STAGES - 1) % STAGES);
+    const uint64_t now = visible(j, p, k0);
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
       f32x16 s[1], dp[1];
@@ -413,24 +520,40 @@ __global__ __launch_bounds__(NT, 1) void xattn_dq_kernel(AttnJob j, int tiles) {
         float pr = __builtin_amdgcn_exp2f(fminf(fmaf(s[0][i], c, -lse), 0.f));   // (scores so far out that the rounding of lse passes 1)
         if (!((bits >> acc_row(i, 0)) & 1)) pr = 0.f;
         s[0][i] = pr * (dp[0][i] - delta);
+        rest += s[0][i];
       }
       dot_cols<T, DP>(dq, kt, 32 * kb, s[0], lane);
     }
   }
-  if (mine) store_row<T, DP>(at<T>(j.dq, j.s.dq, p.b, ro.t, head), dq, j.s.scale, dh, half);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  if (!mine) return;
+  rest = pair_sum(rest);
+  if (sp.parts > 1) {
+    const int64_t row = ((int64_t)w.part * j.s.batch * j.s.kv_heads + w.id) * p.rows + r;
+    if (half == 0) *reinterpret_cast<float2*>(sp.stats + 2 * row) = make_float2(rest, delta);
+    store_row<float, DP>(sp.out[0] + row * dh, dq, 1.f, dh, half);
+    if (w.part == 0 && half == 0) j.row_lse[(int64_t)w.id * p.rows + r] = lse;
+    return;
+  }
+  if (half == 0) {
+    j.row_lse[(int64_t)w.id * p.rows + r] = lse;
+    j.row_delta[(int64_t)w.id * p.rows + r] = delta + rest;
+  }
+  store_row<T, DP>(at<T>(j.dq, j.s.dq, p.b, ro.t, head), dq, j.s.scale, dh, half);
 }
 
 // ---- backward: dk and dv ------------------------------------------------------------------------------
 template <typename T, int DP>
-__global__ __launch_bounds__(NT, 1) void xattn_dkv_kernel(AttnJob j, int tiles) {
-  constexpr int TR = Elem<T>::TR, QB = TR / 32, ELEMS = Tile<T, DP>::ELEMS;
+__global__ __launch_bounds__(NT, DP <= 64 ? 2 : 1) void xattn_dkv_kernel(AttnJob j, AttnSplit sp) {
+  constexpr int TR = Elem<T>::TR, QB = TR / 32, ELEMS = Tile<T, DP>::ELEMS, STAGES = Ring<T, DP>::STAGES, BYTES = Ring<T, DP>::BYTES;
+  constexpr uint64_t ALL = TR == 64 ? ~0ull : (1ull << TR) - 1;
   extern __shared__ __attribute__((aligned(16))) char xattn_lds[];
-  T* lds = reinterpret_cast<T*>(xattn_lds);                 // [2][q, dO][ELEMS], then [2][lse, delta][TR]
-  float* stats = reinterpret_cast<float*>(lds + 4 * ELEMS);
+  T* lds = reinterpret_cast<T*>(xattn_lds);                 // [STAGES][q, dO][ELEMS], then [STAGES][lse, delta][64]
+  float* stats = reinterpret_cast<float*>(lds + 2 * STAGES * ELEMS);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
-  const int id = blockIdx.x / tiles;
-  const Problem p = problem_of(j, id);
-  const int key = (blockIdx.x % tiles) * (4 * WR) + wave * WR + (lane & 31);
+  const Work w = work_of(sp);
+  const Problem p = problem_of(j, w.id);
+  const int key = w.tile * (4 * WR) + wave * WR + (lane & 31);
   const bool mine = key < j.s.k_rows;
   bool seen = key < p.keys;
   if (j.key_mask && seen) seen = j.key_mask[(int64_t)p.b * j.s.k_rows + key] != 0;
@@ -445,35 +568,46 @@ __global__ __launch_bounds__(NT, 1) void xattn_dkv_kernel(AttnJob j, int tiles) 
   clear(dv);
 
   const int rows = p.q_len * j.group;                       // padding lies behind them
-  Stage<T, DP> qs, gs;
-  float stat = 0.f;
-  auto fetch = [&](int r0) {
-    auto row = [&](const void* base, const vf_attn_layout& l, int t) -> const T* {
-      if (r0 + t >= rows) return nullptr;
-      const RowOf ro = row_of(j, r0 + t);
-      return at<const T>(base, l, p.b, ro.t, p.hk * j.group + ro.g);
-    };
-    qs.fetch([&](int t) { return row(j.q, j.s.q, t); }, dh);
-    gs.fetch([&](int t) { return row(j.d_o, j.s.d_o, t); }, dh);
-    const int t = threadIdx.x % TR;
-    if (threadIdx.x < 2 * TR) {
-      const float* from = threadIdx.x < TR ? j.row_lse : j.row_delta;
-      stat = r0 + t < rows ? from[(int64_t)id * p.rows + r0 + t] : (threadIdx.x < TR ? INFINITY : 0.f);
+  const uint32_t lds0 = lds_address(lds) + __builtin_amdgcn_readfirstlane(wave) * 1024, stats0 = lds_address(stats);
+  const char* const zeros = zeros_address();
+  const int beg = w.first * TR, stop = min(rows, beg + sp.per * TR);
+  const int end = w.tile * (4 * WR) < p.keys ? stop : beg;  // (a tile without a visible key: nothing but zeros to write)
+  const uint32_t in_head = Source<T, DP>::head_bits(dh);
+  const int step_t = TR / j.group, step_g = TR % j.group;
+  const int64_t qstep = (step_t * j.s.q.row + step_g * j.s.q.head) * (int64_t)sizeof(T), qover = (j.s.q.row - j.group * j.s.q.head) * (int64_t)sizeof(T);
+  const int64_t gstep = (step_t * j.s.d_o.row + step_g * j.s.d_o.head) * (int64_t)sizeof(T), gover = (j.s.d_o.row - j.group * j.s.d_o.head) * (int64_t)sizeof(T);
+  Source<T, DP> qs, gs;
+  qs.init(j, at<const T>(j.q, j.s.q, p.b, 0, p.hk * j.group), j.s.q, beg, true);
+  gs.init(j, at<const T>(j.d_o, j.s.d_o, p.b, 0, p.hk * j.group), j.s.d_o, beg, true);
+  auto issue = [&](int r0, int buf) {
+    const uint64_t want = first_bits(stop - r0);
+    const bool whole = dh == DP && (want & ALL) == ALL;
+    qs.issue(want, in_head, whole, zeros, lds0 + buf * 2 * BYTES);
+    gs.issue(want, in_head, whole, zeros, lds0 + buf * 2 * BYTES + BYTES);
+    if (step_g == 0) {
+      qs.advance(qstep);
+      gs.advance(gstep);
+    } else {
+      qs.advance(qstep, qover, step_g, j.group);
+      gs.advance(gstep, gover, step_g, j.group);
     }
+    // every wavefront loads the statistics of the 64 rows (the same values to the same place: all count alike)
+    const bool in = r0 + lane < stop;
+    const int64_t at_row = (int64_t)w.id * p.rows + r0 + lane;
+    lds_load4(in ? static_cast<const void*>(j.row_lse + at_row) : &g_infinity, stats0 + buf * 512);
+    lds_load4(in ? static_cast<const void*>(j.row_delta + at_row) : static_cast<const void*>(zeros), stats0 + buf * 512 + 256);
   };
-  const bool block_seen = (blockIdx.x % tiles) * (4 * WR) < p.keys;      // else nothing but zeros to write
-  const int end = block_seen ? rows : 0;
-  if (end > 0) fetch(0);
+  if (beg < end) {
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) issue(beg + i * TR, i);
+  }
   int buf = 0;
-  for (int r0 = 0; r0 < end; r0 += TR, buf ^= 1) {
-    T* qt = lds + buf * 2 * ELEMS;
-    T* gt = qt + ELEMS;
-    float* st = stats + buf * 2 * TR;
-    qs.put(qt);
-    gs.put(gt);
-    if (threadIdx.x < 2 * TR) st[threadIdx.x] = stat;
-    if (r0 + TR < end) fetch(r0 + TR);
-    __syncthreads();
+  for (int r0 = beg; r0 < end; r0 += TR, buf = (buf + 1) % STAGES) {
+    const T* qt = lds + buf * 2 * ELEMS;
+    const T* gt = qt + ELEMS;
+    const float* st = stats + buf * 128;
+    wait_and_meet<(STAGES - 2) * (2 * Ring<T, DP>::N + 2)>();
+    issue(r0 + (STAGES - 1) * TR, (buf + STAGES - 1) % STAGES);
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       f32x16 s[1], dp[1];
@@ -484,7 +618,7 @@ __global__ __launch_bounds__(NT, 1) void xattn_dkv_kernel(AttnJob j, int tiles) 
 #pragma unroll
       for (int gq = 0; gq < 4; ++gq) {
         const f32x4 lse = *reinterpret_cast<const f32x4*>(st + 32 * qb + 8 * gq + 4 * half);
-        const f32x4 delta = *reinterpret_cast<const f32x4*>(st + TR + 32 * qb + 8 * gq + 4 * half);
+        const f32x4 delta = *reinterpret_cast<const f32x4*>(st + 64 + 32 * qb + 8 * gq + 4 * half);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float pr = __builtin_amdgcn_exp2f(fminf(fmaf(s[0][4 * gq + i], c, -lse[i]), 0.f));
@@ -496,11 +630,132 @@ __global__ __launch_bounds__(NT, 1) void xattn_dkv_kernel(AttnJob j, int tiles) 
       dot_cols<T, DP>(dk, qt, 32 * qb, dp[0], lane);
     }
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   if (!mine) return;
   // an invisible key's columns hold what its zeros gave: nothing of it is stored
   if (!seen) { clear(dk); clear(dv); }
+  if (sp.parts > 1) {
+    const int64_t row = ((int64_t)w.part * j.s.batch * j.s.kv_heads + w.id) * j.s.k_rows + key;
+    store_row<float, DP>(sp.out[0] + row * dh, dk, 1.f, dh, half);
+    store_row<float, DP>(sp.out[1] + row * dh, dv, 1.f, dh, half);
+    return;
+  }
   store_row<T, DP>(at<T>(j.dk, j.s.dk, p.b, key, p.hk), dk, j.s.scale, dh, half);
   store_row<T, DP>(at<T>(j.dv, j.s.dv, p.b, key, p.hk), dv, 1.f, dh, half);
+}
+
+// ---- joining the parts -----------------------------------------------------------------------------------
+// A part's rows are fp32 [part][problem][row][d_head].  32 lanes take a row, four elements each; the parts are added in their
+// order.  KIND 0: forward, parts weighed by their maxima and sums; 1: dq, with the rows' delta; 2: dk and 3: dv.
+template <typename T, int KIND>
+__device__ __forceinline__ void join_rows(const AttnJob& j, const AttnSplit& sp, int64_t i, int e) {
+  const int dh = j.s.d_head;
+  const int held = KIND < 2 ? j.group * j.s.q_rows : j.s.k_rows;
+  const int id = (int)((uint32_t)i / (uint32_t)held), r = (int)((uint32_t)i - (uint32_t)id * (uint32_t)held);
+  const int b = id / j.s.kv_heads, hk = id - b * j.s.kv_heads;
+  const int64_t step = (int64_t)j.s.batch * j.s.kv_heads * held;
+  const float* part = sp.out[KIND == 3 ? 1 : 0] + i * dh + e;
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+  float top = -INFINITY, total = 0.f, delta = 0.f, factor = 1.f;
+  if constexpr (KIND == 0) {
+    for (int k = 0; k < sp.parts; ++k) {
+      const float2 ml = *reinterpret_cast<const float2*>(sp.stats + 2 * (i + k * step));
+      if (ml.y != 0.f) top = fmaxf(top, ml.x);
+    }
+    if (top == -INFINITY) top = 0.f;
+  }
+  const float c = j.s.scale * kLog2e;
+  for (int k = 0; k < sp.parts; ++k) {
+    float w = 1.f;
+    if constexpr (KIND < 2) {
+      const float2 st = *reinterpret_cast<const float2*>(sp.stats + 2 * (i + k * step));
+      if constexpr (KIND == 0) {
+        if (st.y == 0.f) continue;                          // (its rows were not written)
+        w = __builtin_amdgcn_exp2f((st.x - top) * c);
+        total = fmaf(st.y, w, total);
+      } else {
+        if (k == 0) delta = st.y;
+        total += st.x;
+      }
+    }
+    if (e < dh) {
+      const float4 v = *reinterpret_cast<const float4*>(part + k * step * dh);
+      sum.x = fmaf(v.x, w, sum.x); sum.y = fmaf(v.y, w, sum.y); sum.z = fmaf(v.z, w, sum.z); sum.w = fmaf(v.w, w, sum.w);
+    }
+  }
+  T* out;
+  if constexpr (KIND < 2) {
+    const RowOf ro = row_of(j, r);
+    const int head = hk * j.group + ro.g;
+    if constexpr (KIND == 0) {
+      out = at<T>(j.o, j.s.o, b, ro.t, head);
+      factor = total != 0.f ? 1.f / total : 0.f;
+      if (j.lse && e == 0)
+        j.lse[((int64_t)b * j.s.q_heads + head) * j.s.q_rows + ro.t] = total != 0.f ? fmaf(top, j.s.scale, logf(total)) : -INFINITY;
+    } else {
+      out = at<T>(j.dq, j.s.dq, b, ro.t, head);
+      factor = j.s.scale;
+      if (e == 0) j.row_delta[i] = delta + total;
+    }
+  } else {
+    out = KIND == 2 ? at<T>(j.dk, j.s.dk, b, r, hk) : at<T>(j.dv, j.s.dv, b, r, hk);
+    factor = KIND == 2 ? j.s.scale : 1.f;
+  }
+  if (e >= dh) return;
+  if constexpr (sizeof(T) == 2) {
+    *reinterpret_cast<uint2*>(out + e) = make_uint2(f32x2_to_bf16x2(sum.x * factor, sum.y * factor), f32x2_to_bf16x2(sum.z * factor, sum.w * factor));
+  } else {
+    *reinterpret_cast<float4*>(out + e) = make_float4(sum.x * factor, sum.y * factor, sum.z * factor, sum.w * factor);
+  }
+}
+template <typename T, int KIND>
+__global__ __launch_bounds__(NT) void xattn_join_kernel(AttnJob j, AttnSplit sp, int64_t rows) {
+  const int64_t i = (int64_t)blockIdx.x * (NT / 32) + (threadIdx.x >> 5);
+  if (i >= rows) return;
+  const int e = 4 * (threadIdx.x & 31);
+  if constexpr (KIND == 2) {
+    if (blockIdx.y == 0) join_rows<T, 2>(j, sp, i, e);
+    else join_rows<T, 3>(j, sp, i, e);
+  } else {
+    join_rows<T, KIND>(j, sp, i, e);
+  }
+}
+
+// How the streamed side is split: one part per tile of held rows where those fill the compute units or the streamed tiles are few;
+// else as many parts as give every unit two workgroups.  Joining costs a launch and a pass over fp32 partial results, about 8 us,
+// a streamed tile 1.2 us (bf16) or 2.5 (fp32): fewer than 8 (4) tiles saved do not pay (192 workgroups of 7 tiles,
+// three parts: 12.6 us of forward became 11.8 + 8.4).
+constexpr int kUnits = 256, kMaxParts = 64;
+AttnSplit split_of(int64_t problems, int held, int streamed, int tile_rows) {
+  const int least_saved = tile_rows == 64 ? 8 : 4;
+  AttnSplit sp{};
+  sp.tiles = (held + 4 * WR - 1) / (4 * WR);
+  const int all = std::max(1, (streamed + tile_rows - 1) / tile_rows);
+  const int64_t groups = problems * sp.tiles;
+  sp.per = all;
+  if (groups > 0 && groups < kUnits) {
+    const int parts = (int)std::min<int64_t>({(2 * kUnits + groups - 1) / groups, (int64_t)all, (int64_t)kMaxParts});
+    const int per = (all + parts - 1) / parts;
+    if (all - per >= least_saved) sp.per = per;
+  }
+  sp.parts = (all + sp.per - 1) / sp.per;
+  return sp;
+}
+int tile_rows_of(const vf_attn_shape& s) { return s.dtype == VF_BF16 ? Elem<bf16_t>::TR : Elem<float>::TR; }
+// The splits of the forward and dq kernels, and of the dk/dv kernel.
+AttnSplit split_rows(const vf_attn_shape& s) {
+  return split_of((int64_t)s.batch * s.kv_heads, s.q_heads / s.kv_heads * s.q_rows, s.k_rows, tile_rows_of(s));
+}
+AttnSplit split_keys(const vf_attn_shape& s) {
+  return split_of((int64_t)s.batch * s.kv_heads, s.k_rows, s.q_heads / s.kv_heads * s.q_rows, tile_rows_of(s));
+}
+int64_t round4(int64_t floats) { return (floats + 3) & ~int64_t(3); }
+// Floats of the parts of a pass over the rows (results and two statistics a row), and over the keys (dk and dv).
+int64_t part_rows_floats(const vf_attn_shape& s, const AttnSplit& sp) {
+  return sp.parts > 1 ? sp.parts * (int64_t)s.batch * s.q_heads * s.q_rows * (s.d_head + 2) : 0;
+}
+int64_t part_keys_floats(const vf_attn_shape& s, const AttnSplit& sp) {
+  return sp.parts > 1 ? sp.parts * (int64_t)s.batch * s.kv_heads * s.k_rows * 2 * s.d_head : 0;
 }
 
 // LDS above 64 KB has to be allowed for a kernel once on every device.
@@ -514,58 +769,99 @@ int allow_lds(const void* kernel, int bytes, std::atomic<uint64_t>& done) {
   return VF_OK;
 }
 
-template <typename T, int DP>
-int launch_fwd(const AttnJob& j, hipStream_t st) {
-  constexpr int lds = 4 * Tile<T, DP>::ELEMS * sizeof(T);
-  static std::atomic<uint64_t> ready{0};
-  VF_TRY(allow_lds(reinterpret_cast<const void*>(&xattn_fwd_kernel<T, DP>), lds, ready));
-  const int tiles = (j.group * j.s.q_rows + 4 * WR - 1) / (4 * WR);
-  xattn_fwd_kernel<T, DP><<<j.s.batch * j.s.kv_heads * tiles, NT, lds, st>>>(j, tiles);
+template <typename T, int KIND>
+int launch_join(const AttnJob& j, const AttnSplit& sp, int64_t rows, hipStream_t st) {
+  xattn_join_kernel<T, KIND><<<dim3((unsigned)((rows + NT / 32 - 1) / (NT / 32)), KIND == 2 ? 2 : 1), NT, 0, st>>>(j, sp, rows);
   VF_LAUNCH_CHECK();
   return VF_OK;
 }
 
 template <typename T, int DP>
-int launch_bwd(const AttnJob& j, hipStream_t st) {
-  constexpr int lds = 4 * Tile<T, DP>::ELEMS * sizeof(T), lds_kv = lds + 4 * Elem<T>::TR * sizeof(float);
+int launch_fwd(const AttnJob& j, float* ws, hipStream_t st) {
+  constexpr int lds = 2 * Ring<T, DP>::STAGES * Ring<T, DP>::BYTES;
+  static std::atomic<uint64_t> ready{0};
+  VF_TRY(allow_lds(reinterpret_cast<const void*>(&xattn_fwd_kernel<T, DP>), lds, ready));
+  const int64_t rows = (int64_t)j.s.batch * j.s.q_heads * j.s.q_rows;
+  AttnSplit sp = split_rows(j.s);
+  sp.out[0] = ws;
+  sp.stats = ws + sp.parts * rows * j.s.d_head;
+  xattn_fwd_kernel<T, DP><<<dim3(j.s.batch * j.s.kv_heads, sp.tiles, sp.parts), NT, lds, st>>>(j, sp);
+  VF_LAUNCH_CHECK();
+  return sp.parts > 1 ? launch_join<T, 0>(j, sp, rows, st) : VF_OK;
+}
+
+template <typename T, int DP>
+int launch_bwd(const AttnJob& j, float* ws, hipStream_t st) {
+  constexpr int lds = 2 * Ring<T, DP>::STAGES * Ring<T, DP>::BYTES, lds_kv = lds + Ring<T, DP>::STAGES * 512;
   static std::atomic<uint64_t> ready_q{0}, ready_kv{0};
   VF_TRY(allow_lds(reinterpret_cast<const void*>(&xattn_dq_kernel<T, DP>), lds, ready_q));
   VF_TRY(allow_lds(reinterpret_cast<const void*>(&xattn_dkv_kernel<T, DP>), lds_kv, ready_kv));
-  const int heads = j.s.batch * j.s.kv_heads;
-  const int qt = (j.group * j.s.q_rows + 4 * WR - 1) / (4 * WR), kt = (j.s.k_rows + 4 * WR - 1) / (4 * WR);
-  if (qt) {
-    xattn_dq_kernel<T, DP><<<heads * qt, NT, lds, st>>>(j, qt);
+  const int problems = j.s.batch * j.s.kv_heads;
+  if (j.s.q_rows) {
+    const int64_t rows = (int64_t)j.s.batch * j.s.q_heads * j.s.q_rows;
+    AttnSplit sp = split_rows(j.s);
+    sp.out[0] = ws;
+    sp.stats = ws + sp.parts * rows * j.s.d_head;
+    xattn_dq_kernel<T, DP><<<dim3(problems, sp.tiles, sp.parts), NT, lds, st>>>(j, sp);
     VF_LAUNCH_CHECK();
+    if (sp.parts > 1) VF_TRY((launch_join<T, 1>(j, sp, rows, st)));
   }
-  if (kt) {
-    xattn_dkv_kernel<T, DP><<<heads * kt, NT, lds_kv, st>>>(j, kt);
+  if (j.s.k_rows) {
+    const int64_t rows = (int64_t)problems * j.s.k_rows;
+    AttnSplit sp = split_keys(j.s);                         // (its parts take the place of the rows' ones)
+    sp.out[0] = ws;
+    sp.out[1] = ws + sp.parts * rows * j.s.d_head;
+    xattn_dkv_kernel<T, DP><<<dim3(problems, sp.tiles, sp.parts), NT, lds_kv, st>>>(j, sp);
     VF_LAUNCH_CHECK();
+    if (sp.parts > 1) VF_TRY((launch_join<T, 2>(j, sp, rows, st)));
   }
   return VF_OK;
 }
 
 }  // namespace
 
-// Backward: two floats per row (lse and rowsum(dO o)).
+// The mask's bits; backward: two floats per row (lse and rowsum(dO o)); then the parts of one pass at a time.
+static int64_t mask_words(const vf_attn_shape& s) { return ((int64_t)s.k_rows + 63) / 64; }
+static int64_t mask_floats(const vf_attn_shape& s) { return round4(2 * s.batch * mask_words(s)); }
 int64_t attn_workspace_bytes(const vf_attn_shape& s, bool backward) {
-  if (!backward) return 0;
-  return (int64_t)s.batch * s.q_heads * s.q_rows * 2 * (int64_t)sizeof(float);
+  if (!s.batch || (!backward && !s.q_rows)) return 0;
+  const int64_t parts = part_rows_floats(s, split_rows(s));
+  if (!backward) return (mask_floats(s) + parts) * (int64_t)sizeof(float);
+  const int64_t stats = 2 * round4((int64_t)s.batch * s.q_heads * s.q_rows);
+  return (mask_floats(s) + stats + std::max(parts, part_keys_floats(s, split_keys(s)))) * (int64_t)sizeof(float);
 }
 
-int launch_attn(const AttnJob& j, void*, hipStream_t st) {
+static int make_bits(AttnJob& j, float* ws, hipStream_t st) {
+  j.words = (int)mask_words(j.s);
+  const int64_t n = (int64_t)j.s.batch * j.words;
+  if (!j.key_mask || !n) return VF_OK;
+  j.bits = reinterpret_cast<uint64_t*>(ws);
+  mask_bits_kernel<<<(unsigned)((n + NT / 64 - 1) / (NT / 64)), NT, 0, st>>>(j.key_mask, j.s.k_rows, j.words, n, reinterpret_cast<uint64_t*>(ws));
+  VF_LAUNCH_CHECK();
+  return VF_OK;
+}
+
+int launch_attn(AttnJob j, void* workspace, hipStream_t st) {
   if (!j.s.batch || !j.s.q_rows) return VF_OK;
+  float* ws = static_cast<float*>(workspace);
+  VF_TRY(make_bits(j, ws, st));
+  ws += mask_floats(j.s);
   const bool wide = j.s.d_head > 64;
-  if (j.s.dtype == VF_BF16) return wide ? launch_fwd<bf16_t, 128>(j, st) : launch_fwd<bf16_t, 64>(j, st);
-  return wide ? launch_fwd<float, 128>(j, st) : launch_fwd<float, 64>(j, st);
+  if (j.s.dtype == VF_BF16) return wide ? launch_fwd<bf16_t, 128>(j, ws, st) : launch_fwd<bf16_t, 64>(j, ws, st);
+  return wide ? launch_fwd<float, 128>(j, ws, st) : launch_fwd<float, 64>(j, ws, st);
 }
 
 int launch_attn_bwd(AttnJob j, void* workspace, hipStream_t st) {
   if (!j.s.batch || (!j.s.q_rows && !j.s.k_rows)) return VF_OK;
-  j.row_lse = static_cast<float*>(workspace);
-  j.row_delta = j.row_lse + (int64_t)j.s.batch * j.s.q_heads * j.s.q_rows;
+  float* ws = static_cast<float*>(workspace);
+  VF_TRY(make_bits(j, ws, st));
+  const int64_t rows = round4((int64_t)j.s.batch * j.s.q_heads * j.s.q_rows);
+  j.row_lse = ws + mask_floats(j.s);
+  j.row_delta = j.row_lse + rows;
+  ws = j.row_delta + rows;
   const bool wide = j.s.d_head > 64;
-  if (j.s.dtype == VF_BF16) return wide ? launch_bwd<bf16_t, 128>(j, st) : launch_bwd<bf16_t, 64>(j, st);
-  return wide ? launch_bwd<float, 128>(j, st) : launch_bwd<float, 64>(j, st);
+  if (j.s.dtype == VF_BF16) return wide ? launch_bwd<bf16_t, 128>(j, ws, st) : launch_bwd<bf16_t, 64>(j, ws, st);
+  return wide ? launch_bwd<float, 128>(j, ws, st) : launch_bwd<float, 64>(j, ws, st);
 }
 
 }  // namespace vf

@@ -580,10 +580,18 @@ struct AttnJob {
   float* lse;
   const void* d_o;
   void *dq, *dk, *dv;
+  const uint64_t* bits; int words;                       // key_mask as bits, `words` words a sample, or null
   float *row_lse, *row_delta;                            // backward: log2-domain lse and rowsum(dO o) of every row, in row order
 };
+// How a kernel's workgroups share the work: `tiles` tiles of held rows, the streamed side in `parts` parts of `per` tiles,
+// whose partial results go to out (and stats) and are joined by a kernel behind it.
+struct AttnSplit {
+  int tiles, parts, per;
+  float* out[2];
+  float* stats;
+};
 int64_t attn_workspace_bytes(const vf_attn_shape& s, bool backward);
-int launch_attn(const AttnJob& j, void* workspace, hipStream_t st);
+int launch_attn(AttnJob j, void* workspace, hipStream_t st);
 int launch_attn_bwd(AttnJob j, void* workspace, hipStream_t st);
 
 }  // namespace vf

@@ -80,12 +80,11 @@ int check_shape(const vf_attn_shape* s) {
   if (!esz || s->batch < 0 || s->q_rows < 0 || s->k_rows < 0 || s->q_heads < 1 || s->kv_heads < 1) return VF_EINVAL;
   if (s->q_heads % s->kv_heads || s->d_head < 8 || s->d_head > 128 || s->d_head % 8) return VF_EINVAL;
   if (!(s->scale > 0.f) || !std::isfinite(s->scale)) return VF_EINVAL;
-  // rows of a problem are found by a multiplication that is exact below this, and workgroups are counted in 32 bits
-  const int64_t group = s->q_heads / s->kv_heads;
-  if (group * group * s->q_rows > INT32_MAX) return VF_EINVAL;
-  const int64_t heads = (int64_t)s->batch * s->kv_heads;
-  const int64_t tiles = std::max<int64_t>({1, (group * s->q_rows + 127) / 128, ((int64_t)s->k_rows + 127) / 128});
-  if (heads > (1 << 23) || heads * tiles > (1 << 23)) return VF_EINVAL;
+  // rows of a problem are found by a multiplication that is exact below this; problems and tiles of 128 rows are dimensions of
+  // a grid, joined rows are counted in 32 bits
+  const int64_t group = s->q_heads / s->kv_heads, problems = (int64_t)s->batch * s->kv_heads;
+  const int64_t rows = std::max<int64_t>(group * s->q_rows, s->k_rows);
+  if (group * group * s->q_rows > INT32_MAX || rows > 128 * 65535 || problems > (1 << 23) || problems * rows > INT32_MAX) return VF_EINVAL;
   return VF_OK;
 }
 
