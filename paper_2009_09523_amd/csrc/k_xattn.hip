@@ -77,23 +77,54 @@ struct Held {
       if (row && e < dh) w[s] = *reinterpret_cast<const u32x4*>(row + e);
     }
   }
+  // Waits for the loads here: the compiler does not count the loads of tiles, and would wait for all of them at the first use
+  // of w in the loop, in every iteration.
+  __device__ __forceinline__ void arrive() {
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) asm volatile("" : "+v"(w[s]));
+  }
 };
 
-// acc[streamed row][held column] += tile rows row0 .. row0 + 31 times the held rows, over the head.
-template <typename T, int DP>
-__device__ __forceinline__ void dot_rows(f32x16& acc, const T* tile, int row0, const Held<T, DP>& b, int lane) {
-  const int r = row0 + (lane & 31), half = lane >> 5;
+// acc[streamed row][held column] = 32 tile rows times the held rows, over the head; two such products at once (rows ra of tile ta
+// with a, rows rb of tile tb with b), their operations in turn.  The operands are asked for AHEAD steps ahead of their use:
+// left to itself the compiler waits for every one of them just before the instruction that takes it.
+template <typename T>
+__device__ __forceinline__ void step_of(f32x16& acc, u32x4 x, u32x4 y) {
+  if constexpr (sizeof(T) == 2) {
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), acc, 0, 0, 0);
+  } else {
+    const f32x4 u = __builtin_bit_cast(f32x4, x), v = __builtin_bit_cast(f32x4, y);
 #pragma unroll
-  for (int s = 0; s < Held<T, DP>::STEPS; ++s) {
-    const u32x4 a = *reinterpret_cast<const u32x4*>(tile + Tile<T, DP>::pos(r, 2 * s + half));
-    if constexpr (sizeof(T) == 2) {
-      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b.w[s]), acc, 0, 0, 0);
-    } else {
-      const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b.w[s]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], y[e], acc, 0, 0, 0);
-    }
+    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(u[e], v[e], acc, 0, 0, 0);
   }
+}
+template <typename T, int DP, bool TWO, int AHEAD = 4>
+__device__ __forceinline__ void dot_rows(f32x16& accA, const T* ta, int ra, const Held<T, DP>& a, f32x16& accB, const T* tb, int rb,
+                                         const Held<T, DP>& b, int lane) {
+  constexpr int S = Held<T, DP>::STEPS, LOOK = S < AHEAD ? S : AHEAD, PAIR = TWO ? 2 : 1, OPS = PAIR * (sizeof(T) == 2 ? 1 : 4);
+  const int half = lane >> 5;
+  ra += lane & 31;
+  rb += lane & 31;
+  u32x4 x[S], y[S];
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+    x[s] = *reinterpret_cast<const u32x4*>(ta + Tile<T, DP>::pos(ra, 2 * s + half));
+    if constexpr (TWO) y[s] = *reinterpret_cast<const u32x4*>(tb + Tile<T, DP>::pos(rb, 2 * s + half));
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) accA[i] = accB[i] = 0.f;
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+    step_of<T>(accA, x[s], a.w[s]);
+    if constexpr (TWO) step_of<T>(accB, y[s], b.w[s]);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x100, PAIR * LOOK, 0);     // LDS reads
+#pragma unroll
+  for (int s = 0; s < S - LOOK; ++s) {
+    __builtin_amdgcn_sched_group_barrier(0x8, OPS, 0);             // matrix instructions
+    __builtin_amdgcn_sched_group_barrier(0x100, PAIR, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x8, OPS * LOOK, 0);
 }
 
 // Transposing read: elements (row0 + 4 half + 0..3, col0 + l % 32) and the same eight rows further down.
@@ -299,8 +330,13 @@ __global__ __launch_bounds__(NT) void mask_bits_kernel(const uint8_t* __restrict
 }
 
 // max / sum over the two lanes of a column
-__device__ __forceinline__ float pair_max(float v) { return fmaxf(v, __shfl_xor(v, 32, 64)); }
-__device__ __forceinline__ float pair_sum(float v) { return v + __shfl_xor(v, 32, 64); }
+__device__ __forceinline__ float other_half(float v, float* mine) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  *mine = __uint_as_float(r[0]);                            // (in both halves: the lower lane's, the upper lane's)
+  return __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float pair_max(float v) { float a; const float b = other_half(v, &a); return fmaxf(a, b); }
+__device__ __forceinline__ float pair_sum(float v) { float a; const float b = other_half(v, &a); return a + b; }
 
 // An accumulator over the head (elements down, held rows across), times `f`, to the lane's row.
 template <typename T, int DP>
@@ -340,7 +376,6 @@ __global__ __launch_bounds__(NT, 2) void xattn_fwd_kernel(AttnJob j, AttnSplit s
   const float c = j.s.scale * kLog2e;
 
   Held<T, DP> q;
-  q.load(live ? at<const T>(j.q, j.s.q, p.b, ro.t, head) : nullptr, dh, half);
   f32x16 o[DP / 32];
   clear(o);
   float m = -INFINITY, l = 0.f;
@@ -364,6 +399,8 @@ __global__ __launch_bounds__(NT, 2) void xattn_fwd_kernel(AttnJob j, AttnSplit s
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) issue(kbeg + i * TR, i);
   }
+  q.load(live ? at<const T>(j.q, j.s.q, p.b, ro.t, head) : nullptr, dh, half);
+  q.arrive();
   int buf = 0;
   for (int k0 = kbeg; k0 < kend; k0 += TR, buf = (buf + 1) % STAGES) {
     const T* kt = lds + buf * 2 * ELEMS;
@@ -372,9 +409,12 @@ __global__ __launch_bounds__(NT, 2) void xattn_fwd_kernel(AttnJob j, AttnSplit s
     issue(k0 + (STAGES - 1) * TR, (buf + STAGES - 1) % STAGES);
     const uint64_t now = visible(j, p, k0);
     f32x16 s[KB];
-    clear(s);
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) dot_rows<T, DP>(s[kb], kt, 32 * kb, q, lane);
+    if constexpr (KB == 2) {
+      dot_rows<T, DP, true>(s[0], kt, 0, q, s[1], kt, 32, q, lane);
+    } else {
+      f32x16 none;
+      dot_rows<T, DP, false>(s[0], kt, 0, q, none, kt, 0, q, lane);
+    }
     if ((now & ALL) != ALL) {
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
@@ -413,10 +453,12 @@ __global__ __launch_bounds__(NT, 2) void xattn_fwd_kernel(AttnJob j, AttnSplit s
 #pragma unroll
       for (int i = 0; i < 16; ++i) sum += s[kb][i];
     l = l * fade + sum;
+    if (__any(fade != 1.f)) {                               // (most tiles bring no row a new maximum)
 #pragma unroll
-    for (int db = 0; db < DP / 32; ++db)
+      for (int db = 0; db < DP / 32; ++db)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[db][i] *= fade;
+        for (int i = 0; i < 16; ++i) o[db][i] *= fade;
+    }
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) dot_cols<T, DP>(o, vt, 32 * kb, s[kb], lane);
   }
@@ -438,7 +480,7 @@ __global__ __launch_bounds__(NT, 2) void xattn_fwd_kernel(AttnJob j, AttnSplit s
 
 // ---- backward: dq, and lse / rowsum(dO o) of every row for the kernel behind it ---------------------
 template <typename T, int DP>
-__global__ __launch_bounds__(NT, DP <= 64 ? 2 : 1) void xattn_dq_kernel(AttnJob j, AttnSplit sp) {
+__global__ __launch_bounds__(NT, DP * sizeof(T) <= 256 ? 2 : 1) void xattn_dq_kernel(AttnJob j, AttnSplit sp) {
   constexpr int TR = Elem<T>::TR, KB = TR / 32, ELEMS = Tile<T, DP>::ELEMS, STAGES = Ring<T, DP>::STAGES, BYTES = Ring<T, DP>::BYTES;
   constexpr uint64_t ALL = TR == 64 ? ~0ull : (1ull << TR) - 1;
   extern __shared__ __attribute__((aligned(16))) char xattn_lds[];
@@ -457,26 +499,6 @@ __global__ __launch_bounds__(NT, DP <= 64 ? 2 : 1) void xattn_dq_kernel(AttnJob 
   const bool live = lse_in != -INFINITY;                    // a row without a visible key has p = 0 everywhere
   const float lse = live ? lse_in * kLog2e : INFINITY;
 
-  Held<T, DP> q, g;
-  q.load(live ? at<const T>(j.q, j.s.q, p.b, ro.t, head) : nullptr, dh, half);
-  g.load(live ? at<const T>(j.d_o, j.s.d_o, p.b, ro.t, head) : nullptr, dh, half);
-  float delta = 0.f;
-  {
-    Held<T, DP> out;
-    out.load(live ? at<const T>(j.o, j.s.o, p.b, ro.t, head) : nullptr, dh, half);
-#pragma unroll
-    for (int s = 0; s < Held<T, DP>::STEPS; ++s)
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        if constexpr (sizeof(T) == 2) {
-          delta = fmaf(__uint_as_float(out.w[s][u] << 16), __uint_as_float(g.w[s][u] << 16), delta);
-          delta = fmaf(__uint_as_float(out.w[s][u] & 0xffff0000u), __uint_as_float(g.w[s][u] & 0xffff0000u), delta);
-        } else {
-          delta = fmaf(__uint_as_float(out.w[s][u]), __uint_as_float(g.w[s][u]), delta);
-        }
-      }
-    delta = pair_sum(delta);
-  }
   f32x16 dq[DP / 32];
   clear(dq);
   float rest = 0.f;                                         // sum of dz: 0 with the exact rowsum, here the error of o's rounding
@@ -500,6 +522,28 @@ __global__ __launch_bounds__(NT, DP <= 64 ? 2 : 1) void xattn_dq_kernel(AttnJob 
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) issue(kbeg + i * TR, i);
   }
+  Held<T, DP> q, g;
+  q.load(live ? at<const T>(j.q, j.s.q, p.b, ro.t, head) : nullptr, dh, half);
+  g.load(live ? at<const T>(j.d_o, j.s.d_o, p.b, ro.t, head) : nullptr, dh, half);
+  float delta = 0.f;
+  {
+    Held<T, DP> out;
+    out.load(live ? at<const T>(j.o, j.s.o, p.b, ro.t, head) : nullptr, dh, half);
+#pragma unroll
+    for (int s = 0; s < Held<T, DP>::STEPS; ++s)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if constexpr (sizeof(T) == 2) {
+          delta = fmaf(__uint_as_float(out.w[s][u] << 16), __uint_as_float(g.w[s][u] << 16), delta);
+          delta = fmaf(__uint_as_float(out.w[s][u] & 0xffff0000u), __uint_as_float(g.w[s][u] & 0xffff0000u), delta);
+        } else {
+          delta = fmaf(__uint_as_float(out.w[s][u]), __uint_as_float(g.w[s][u]), delta);
+        }
+      }
+    delta = pair_sum(delta);
+  }
+  q.arrive();
+  g.arrive();
   int buf = 0;
   for (int k0 = kbeg; k0 < kend; k0 += TR, buf = (buf + 1) % STAGES) {
     const T* kt = lds + buf * 2 * ELEMS;
@@ -507,13 +551,10 @@ __global__ __launch_bounds__(NT, DP <= 64 ? 2 : 1) void xattn_dq_kernel(AttnJob 
     wait_and_meet<(STAGES - 2) * 2 * Ring<T, DP>::N>();     // this tile is there, and nobody reads the one before it
     issue(k0 + (STAGES - 1) * TR, (buf + STAGES - 1) % STAGES);
     const uint64_t now = visible(j, p, k0);
-#pragma unroll
+#pragma unroll 1
     for (int kb = 0; kb < KB; ++kb) {
       f32x16 s[1], dp[1];
-      clear(s);
-      clear(dp);
-      dot_rows<T, DP>(s[0], kt, 32 * kb, q, lane);
-      dot_rows<T, DP>(dp[0], vt, 32 * kb, g, lane);
+      dot_rows<T, DP, true, 2>(s[0], kt, 32 * kb, q, dp[0], vt, 32 * kb, g, lane);
       const uint32_t bits = (uint32_t)(now >> (32 * kb)) >> (4 * half);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -544,7 +585,7 @@ __global__ __launch_bounds__(NT, DP <= 64 ? 2 : 1) void xattn_dq_kernel(AttnJob 
 
 // ---- backward: dk and dv ------------------------------------------------------------------------------
 template <typename T, int DP>
-__global__ __launch_bounds__(NT, DP <= 64 ? 2 : 1) void xattn_dkv_kernel(AttnJob j, AttnSplit sp) {
+__global__ __launch_bounds__(NT, DP * sizeof(T) <= 128 ? 2 : 1) void xattn_dkv_kernel(AttnJob j, AttnSplit sp) {
   constexpr int TR = Elem<T>::TR, QB = TR / 32, ELEMS = Tile<T, DP>::ELEMS, STAGES = Ring<T, DP>::STAGES, BYTES = Ring<T, DP>::BYTES;
   constexpr uint64_t ALL = TR == 64 ? ~0ull : (1ull << TR) - 1;
   extern __shared__ __attribute__((aligned(16))) char xattn_lds[];
@@ -561,8 +602,6 @@ __global__ __launch_bounds__(NT, DP <= 64 ? 2 : 1) void xattn_dkv_kernel(AttnJob
   const float c = j.s.scale * kLog2e;
 
   Held<T, DP> k, v;
-  k.load(seen ? at<const T>(j.k, j.s.k, p.b, key, p.hk) : nullptr, dh, half);
-  v.load(seen ? at<const T>(j.v, j.s.v, p.b, key, p.hk) : nullptr, dh, half);
   f32x16 dk[DP / 32], dv[DP / 32];
   clear(dk);
   clear(dv);
@@ -601,6 +640,10 @@ __global__ __launch_bounds__(NT, DP <= 64 ? 2 : 1) void xattn_dkv_kernel(AttnJob
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) issue(beg + i * TR, i);
   }
+  k.load(seen ? at<const T>(j.k, j.s.k, p.b, key, p.hk) : nullptr, dh, half);
+  v.load(seen ? at<const T>(j.v, j.s.v, p.b, key, p.hk) : nullptr, dh, half);
+  k.arrive();
+  v.arrive();
   int buf = 0;
   for (int r0 = beg; r0 < end; r0 += TR, buf = (buf + 1) % STAGES) {
     const T* qt = lds + buf * 2 * ELEMS;
@@ -611,10 +654,7 @@ __global__ __launch_bounds__(NT, DP <= 64 ? 2 : 1) void xattn_dkv_kernel(AttnJob
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       f32x16 s[1], dp[1];
-      clear(s);
-      clear(dp);
-      dot_rows<T, DP>(s[0], qt, 32 * qb, k, lane);
-      dot_rows<T, DP>(dp[0], gt, 32 * qb, v, lane);
+      dot_rows<T, DP, true>(s[0], qt, 32 * qb, k, dp[0], gt, 32 * qb, v, lane);
 #pragma unroll
       for (int gq = 0; gq < 4; ++gq) {
         const f32x4 lse = *reinterpret_cast<const f32x4*>(st + 32 * qb + 8 * gq + 4 * half);
