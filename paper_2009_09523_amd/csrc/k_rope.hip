@@ -22,24 +22,35 @@ struct Turns { double t[VF_ROPE_MAX_PAIRS]; };
 
 template <typename T, int C> struct Chunk;
 template <> struct Chunk<float, 4> {
-  static __device__ __forceinline__ void load(const float* p, float* v) { *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(p); }
-  static __device__ __forceinline__ void store(float* p, const float* v) { *reinterpret_cast<float4*>(p) = *reinterpret_cast<const float4*>(v); }
+  typedef vf_f32x4 Raw;
+  static __device__ __forceinline__ Raw zero() { return Raw{0.f, 0.f, 0.f, 0.f}; }
+  static __device__ __forceinline__ Raw load(const float* p) { return *reinterpret_cast<const Raw*>(p); }
+  static __device__ __forceinline__ void open(const Raw& r, float* v) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = r[u];
+  }
+  static __device__ __forceinline__ void store(float* p, const float* v) { *reinterpret_cast<Raw*>(p) = Raw{v[0], v[1], v[2], v[3]}; }
 };
 template <> struct Chunk<bf16_t, 8> {
-  static __device__ __forceinline__ void load(const bf16_t* p, float* v) {
-    const vf_u32x4 w = *reinterpret_cast<const vf_u32x4*>(p);
+  typedef vf_u32x4 Raw;
+  static __device__ __forceinline__ Raw zero() { return Raw{0u, 0u, 0u, 0u}; }
+  static __device__ __forceinline__ Raw load(const bf16_t* p) { return *reinterpret_cast<const Raw*>(p); }
+  static __device__ __forceinline__ void open(const Raw& w, float* v) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) { v[2 * u] = __uint_as_float(w[u] << 16); v[2 * u + 1] = __uint_as_float(w[u] & 0xffff0000u); }
   }
   static __device__ __forceinline__ void store(bf16_t* p, const float* v) {
-    vf_u32x4 w;
+    Raw w;
 #pragma unroll
     for (int u = 0; u < 4; ++u) w[u] = f32x2_to_bf16x2(v[2 * u], v[2 * u + 1]);
-    *reinterpret_cast<vf_u32x4*>(p) = w;
+    *reinterpret_cast<Raw*>(p) = w;
   }
 };
 template <typename T> struct Chunk<T, 1> {
-  static __device__ __forceinline__ void load(const T* p, float* v) { v[0] = load_f(p); }
+  typedef float Raw;
+  static __device__ __forceinline__ Raw zero() { return 0.f; }
+  static __device__ __forceinline__ Raw load(const T* p) { return load_f(p); }
+  static __device__ __forceinline__ void open(const Raw& r, float* v) { v[0] = r; }
   static __device__ __forceinline__ void store(T* p, const float* v) { store_f(p, v[0]); }
 };
 
@@ -146,11 +157,15 @@ __device__ __forceinline__ float lanes_sum(float v, int lanes) {
   return v;
 }
 
+// A thread asks for the chunks of AHEAD heads before it works on the first of them, and for the first ones before the angles
+// are taken.  (65536 rows of 16 heads of 128, bf16, half of each turned: one head after the other 116 us.)
 template <typename T, int C, int NS, bool NORM>
 __global__ __launch_bounds__(NT) void rope_kernel(RopeJob j, Turns turns) {
+  constexpr int AHEAD = NS > 1 ? 1 : NORM ? 2 : 4;
+  typedef Chunk<T, C> Ch;
   extern __shared__ float2 rope_cs[];
   const HeadBlock hb = head_block(j, blockIdx.y);
-  const int lanes = 1 << j.lane_bits, me = threadIdx.x & (lanes - 1), units = NT >> j.lane_bits;
+  const int lanes = 1 << j.lane_bits, me = threadIdx.x & (lanes - 1), units = NT >> j.lane_bits, unit = threadIdx.x >> j.lane_bits;
   Slot k[NS];
   float g0[NS][C], g1[NS][C];
 #pragma unroll
@@ -167,42 +182,60 @@ __global__ __launch_bounds__(NT) void rope_kernel(RopeJob j, Turns turns) {
   }
   for (int64_t row0 = (int64_t)blockIdx.x * j.tile; row0 < j.rows; row0 += (int64_t)gridDim.x * j.tile) {
     const int rows = (int)min((int64_t)j.tile, j.rows - row0);
-    if (j.rot) {
-      __syncthreads();                                   // the last tile's cosines are no longer read
-      fill_angles(j, turns, row0, rows, rope_cs);
-      __syncthreads();
-    }
     const int items = rows * hb.count;
-    for (int base = 0; base < items; base += units) {
-      const int item = base + (threadIdx.x >> j.lane_bits);
-      const bool on = item < items;
-      const int r = on ? item / hb.count : 0, h = on ? item - r * hb.count : 0;
-      const T* x = static_cast<const T*>(j.x) + (row0 + r) * j.x_row + (int64_t)(hb.first + h) * j.x_head;
-      T* y = static_cast<T*>(j.y) + (row0 + r) * j.y_row + (int64_t)(hb.first + h) * j.y_head;
-      float v0[NS][C], v1[NS][C], ss = 0.f;
-  #pragma unroll
-      for (int i = 0; i < NS; ++i) {
-  #pragma unroll
-        for (int e = 0; e < C; ++e) v0[i][e] = v1[i][e] = 0.f;
-        if (on && k[i].a0 >= 0) Chunk<T, C>::load(x + k[i].a0, v0[i]);
-        if (on && k[i].a1 >= 0) Chunk<T, C>::load(x + k[i].a1, v1[i]);
-        if constexpr (NORM) {
-  #pragma unroll
-          for (int e = 0; e < C; ++e) ss += v0[i][e] * v0[i][e] + v1[i][e] * v1[i][e];
+    const uint32_t inv = 0xffffffffu / (uint32_t)hb.count + 1;   // exact: item hb.count < 2^32
+    const T* xt = static_cast<const T*>(j.x) + row0 * j.x_row + (int64_t)hb.first * j.x_head;
+    T* yt = static_cast<T*>(j.y) + row0 * j.y_row + (int64_t)hb.first * j.y_head;
+    for (int base = unit; base - unit < items; base += units * AHEAD) {
+      typename Ch::Raw x0[AHEAD][NS], x1[AHEAD][NS];
+      int r[AHEAD], h[AHEAD];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int item = base + u * units;
+        if (u && base - unit + u * units >= items) break;  // (nothing left for any thread)
+        r[u] = hb.count == 1 ? item : (int)__umulhi((uint32_t)item, inv);   // item / hb.count
+        h[u] = item - r[u] * hb.count;
+        const T* x = xt + r[u] * j.x_row + h[u] * j.x_head;
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+          x0[u][i] = item < items && k[i].a0 >= 0 ? Ch::load(x + k[i].a0) : Ch::zero();
+          x1[u][i] = item < items && k[i].a1 >= 0 ? Ch::load(x + k[i].a1) : Ch::zero();
         }
       }
-      if constexpr (NORM) {
-        const float rstd = 1.0f / sqrtf(lanes_sum(ss, lanes) / (float)j.dh + j.eps);
-  #pragma unroll
-        for (int i = 0; i < NS; ++i)
-  #pragma unroll
-          for (int e = 0; e < C; ++e) { v0[i][e] *= rstd * g0[i][e]; v1[i][e] *= rstd * g1[i][e]; }
+      if (j.rot && base == unit) {                         // (every thread's first turn)
+        __syncthreads();                                   // the last tile's cosines are no longer read
+        fill_angles(j, turns, row0, rows, rope_cs);
+        __syncthreads();
       }
-  #pragma unroll
-      for (int i = 0; i < NS; ++i) {
-        turn_slot<C>(k[i], rope_cs + r * (j.rot / 2), v0[i], v1[i]);
-        if (on && k[i].a0 >= 0) Chunk<T, C>::store(y + k[i].a0, v0[i]);
-        if (on && k[i].a1 >= 0) Chunk<T, C>::store(y + k[i].a1, v1[i]);
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        if (u && base - unit + u * units >= items) break;
+        const bool on = base + u * units < items;
+        float v0[NS][C], v1[NS][C], ss = 0.f;
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+          Ch::open(x0[u][i], v0[i]);
+          Ch::open(x1[u][i], v1[i]);
+          if constexpr (NORM) {
+#pragma unroll
+            for (int e = 0; e < C; ++e) ss += v0[i][e] * v0[i][e] + v1[i][e] * v1[i][e];
+          }
+        }
+        if constexpr (NORM) {
+          const float rstd = 1.0f / sqrtf(lanes_sum(ss, lanes) / (float)j.dh + j.eps);
+#pragma unroll
+          for (int i = 0; i < NS; ++i)
+#pragma unroll
+            for (int e = 0; e < C; ++e) { v0[i][e] *= rstd * g0[i][e]; v1[i][e] *= rstd * g1[i][e]; }
+        }
+        T* y = yt + r[u] * j.y_row + h[u] * j.y_head;
+        const float2* cs = rope_cs + (on ? r[u] : 0) * (j.rot / 2);
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+          turn_slot<C>(k[i], cs, v0[i], v1[i]);
+          if (on && k[i].a0 >= 0) Ch::store(y + k[i].a0, v0[i]);
+          if (on && k[i].a1 >= 0) Ch::store(y + k[i].a1, v1[i]);
+        }
       }
     }
   }
@@ -212,6 +245,7 @@ __global__ __launch_bounds__(NT) void rope_kernel(RopeJob j, Turns turns) {
 // partial sums of dgamma stay few; they are added in the order of the workgroups by gamma_finish_kernel.
 template <typename T, int C, int NS>
 __global__ __launch_bounds__(NT) void norm_bwd_kernel(RopeJob j, Turns turns) {
+  typedef Chunk<T, C> Ch;
   extern __shared__ float2 rope_cs[];
   const HeadBlock hb = head_block(j, blockIdx.y);
   const int lanes = 1 << j.lane_bits, me = threadIdx.x & (lanes - 1), units = NT >> j.lane_bits, unit = threadIdx.x >> j.lane_bits;
@@ -230,30 +264,37 @@ __global__ __launch_bounds__(NT) void norm_bwd_kernel(RopeJob j, Turns turns) {
   }
   for (int64_t row0 = (int64_t)blockIdx.x * j.tile; row0 < j.rows; row0 += (int64_t)gridDim.x * j.tile) {
     const int rows = (int)min((int64_t)j.tile, j.rows - row0);
-    if (j.rot) {
-      __syncthreads();                                   // the last tile's cosines are no longer read
-      fill_angles(j, turns, row0, rows, rope_cs);
-      __syncthreads();
-    }
     const int items = rows * hb.count;
+    const uint32_t inv = 0xffffffffu / (uint32_t)hb.count + 1;   // exact: item hb.count < 2^32
     for (int base = 0; base < items; base += units) {
       const int item = base + unit;
       const bool on = item < items;
-      const int r = on ? item / hb.count : 0, h = on ? item - r * hb.count : 0;
+      const int r = on ? (hb.count == 1 ? item : (int)__umulhi((uint32_t)item, inv)) : 0, h = on ? item - r * hb.count : 0;
       const int64_t row = row0 + r, head = hb.first + h;
       const T* x = static_cast<const T*>(j.x) + row * j.x_row + head * j.x_head;
       const T* dy = static_cast<const T*>(j.dy) + row * j.dy_row + head * j.dy_head;
       T* dx = static_cast<T*>(j.y) + row * j.y_row + head * j.y_head;
+      typename Ch::Raw rx0[NS], rx1[NS], rd0[NS], rd1[NS];
+#pragma unroll
+      for (int i = 0; i < NS; ++i) {
+        const bool p0 = on && k[i].a0 >= 0, p1 = on && k[i].a1 >= 0;
+        rx0[i] = p0 ? Ch::load(x + k[i].a0) : Ch::zero();
+        rx1[i] = p1 ? Ch::load(x + k[i].a1) : Ch::zero();
+        rd0[i] = p0 ? Ch::load(dy + k[i].a0) : Ch::zero();
+        rd1[i] = p1 ? Ch::load(dy + k[i].a1) : Ch::zero();
+      }
+      if (j.rot && base == 0) {                            // (the loads are under way meanwhile)
+        __syncthreads();                                   // the last tile's cosines are no longer read
+        fill_angles(j, turns, row0, rows, rope_cs);
+        __syncthreads();
+      }
       float x0[NS][C], x1[NS][C], d0[NS][C], d1[NS][C], ss = 0.f, hx = 0.f;
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
-#pragma unroll
-        for (int e = 0; e < C; ++e) x0[i][e] = x1[i][e] = d0[i][e] = d1[i][e] = 0.f;
-        if (on && k[i].a0 >= 0) { Chunk<T, C>::load(x + k[i].a0, x0[i]); Chunk<T, C>::load(dy + k[i].a0, d0[i]); }
-        if (on && k[i].a1 >= 0) { Chunk<T, C>::load(x + k[i].a1, x1[i]); Chunk<T, C>::load(dy + k[i].a1, d1[i]); }
-      }
-#pragma unroll
-      for (int i = 0; i < NS; ++i) {
+        Ch::open(rx0[i], x0[i]);
+        Ch::open(rx1[i], x1[i]);
+        Ch::open(rd0[i], d0[i]);
+        Ch::open(rd1[i], d1[i]);
         turn_slot<C>(k[i], rope_cs + r * (j.rot / 2), d0[i], d1[i]);
 #pragma unroll
         for (int e = 0; e < C; ++e) {
@@ -274,13 +315,14 @@ __global__ __launch_bounds__(NT) void norm_bwd_kernel(RopeJob j, Turns turns) {
           d0[i][e] = rstd * (d0[i][e] * g0[i][e] - xh0 * mean);
           d1[i][e] = rstd * (d1[i][e] * g1[i][e] - xh1 * mean);
         }
-        if (on && k[i].a0 >= 0) Chunk<T, C>::store(dx + k[i].a0, d0[i]);
-        if (on && k[i].a1 >= 0) Chunk<T, C>::store(dx + k[i].a1, d1[i]);
+        if (on && k[i].a0 >= 0) Ch::store(dx + k[i].a0, d0[i]);
+        if (on && k[i].a1 >= 0) Ch::store(dx + k[i].a1, d1[i]);
       }
     }
   }
   if (!j.partial) return;
-  // the units' sums side by side in LDS, then one column per thread in the order of the units
+  // The units' sums side by side in LDS; then 256 threads take the columns, several groups of units to a column where there are
+  // fewer than 256, each group in the order of its units, and the groups in theirs.
   float* sums = reinterpret_cast<float*>(rope_cs);
   __syncthreads();
 #pragma unroll
@@ -292,10 +334,25 @@ __global__ __launch_bounds__(NT) void norm_bwd_kernel(RopeJob j, Turns turns) {
     }
   __syncthreads();
   float* out = j.partial + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * j.dh;
-  for (int c = threadIdx.x; c < j.dh; c += NT) {
+  const int groups = max(1, min(units, NT / j.dh)), per = (units + groups - 1) / groups;
+  for (int c0 = 0; c0 < j.dh; c0 += NT) {
+    const int g = groups > 1 ? (int)threadIdx.x / j.dh : 0, c = c0 + (groups > 1 ? (int)threadIdx.x - g * j.dh : (int)threadIdx.x);
     float v = 0.f;
-    for (int u = 0; u < units; ++u) v += sums[u * j.dh + c];
-    out[c] = v;
+    if (c < j.dh && g < groups) {
+      const int first = g * per, last = min(units, first + per);
+#pragma unroll 8
+      for (int u = first; u < last; ++u) v += sums[u * j.dh + c];
+    }
+    if (groups > 1) {                                      // (then c0 is 0: one turn)
+      __syncthreads();
+      if (c < j.dh && g < groups) sums[g * j.dh + c] = v;
+      __syncthreads();
+      if (g == 0 && c < j.dh) {
+        v = 0.f;
+        for (int i = 0; i < groups; ++i) v += sums[i * j.dh + c];
+      }
+    }
+    if (g == 0 && c < j.dh) out[c] = v;
   }
 }
 

@@ -37,21 +37,23 @@ __device__ __forceinline__ int acc_row(int r, int half) { return 8 * (r >> 2) + 
 template <typename T> struct Elem;
 template <> struct Elem<bf16_t> {
   static constexpr int CE = 8;                              // elements of a 16-byte chunk
-  static constexpr int TR = 64;                             // rows of a streamed tile
+  static constexpr int TR = 64;                             // rows of a streamed tile, at least
 };
 template <> struct Elem<float> {
   static constexpr int CE = 4;
   static constexpr int TR = 32;
 };
+// The four wavefronts of a workgroup hold 4 / SW blocks of 32 rows; the SW wavefronts that hold the same block take
+// different blocks of 32 streamed rows of a tile, and their results are joined at the end.
+template <typename T, int SW> constexpr int tile_rows() { return Elem<T>::TR > 32 * SW ? Elem<T>::TR : 32 * SW; }
 
-// A streamed tile in LDS: TR rows of DP elements, unpadded; chunk c of row r lies at position c ^ f(r) of its row, f chosen
+// A streamed tile in LDS: rows of DP elements, unpadded; chunk c of row r lies at position c ^ f(r) of its row, f chosen
 // so that 16 consecutive rows put equal chunks on 16 different 16-byte columns of the banks, and four consecutive
 // rows put four neighbouring chunks on different ones (the transposing read).
 template <typename T, int DP>
 struct Tile {
-  static constexpr int CE = Elem<T>::CE, TR = Elem<T>::TR;
+  static constexpr int CE = Elem<T>::CE;
   static constexpr int CH = DP / CE;                        // chunks of a row
-  static constexpr int ELEMS = TR * DP;
   static_assert(CH % 4 == 0, "chunks of a row");
   static __device__ __forceinline__ int pos(int r, int c) {
     int f;
@@ -143,23 +145,31 @@ __device__ __forceinline__ bf16x8 read_cols(const bf16_t* tile, int row0, int co
 }
 
 // acc[db][head element 32 db + ..][held column] += sum over tile rows row0 .. row0 + 31 of tile[row][element] w[row][column].
-// w is an accumulator tile; bf16 rounds it (the operand of a product).
-template <typename T, int DP>
-__device__ __forceinline__ void dot_cols(f32x16 (&acc)[DP / 32], const T* tile, int row0, const f32x16& w, int lane) {
+// w is an accumulator tile; bf16 rounds it (the operand of a product).  With TWO, acc2 += the same rows times w2.
+template <typename T, int DP, bool TWO = false>
+__device__ __forceinline__ void dot_cols(f32x16 (&acc)[DP / 32], const T* tile, int row0, const f32x16& w, int lane,
+                                         f32x16 (*acc2)[DP / 32] = nullptr, const f32x16* w2 = nullptr) {
   if constexpr (sizeof(T) == 2) {
-    bf16x8 b[2];
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
+    auto operand = [](const f32x16& v, int s) {
       u32x4 packed;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) packed[u] = f32x2_to_bf16x2(w[8 * s + 2 * u], w[8 * s + 2 * u + 1]);
-      b[s] = __builtin_bit_cast(bf16x8, packed);
+      for (int u = 0; u < 4; ++u) packed[u] = f32x2_to_bf16x2(v[8 * s + 2 * u], v[8 * s + 2 * u + 1]);
+      return __builtin_bit_cast(bf16x8, packed);
+    };
+    bf16x8 b[2], b2[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      b[s] = operand(w, s);
+      if constexpr (TWO) b2[s] = operand(*w2, s);
     }
 #pragma unroll
     for (int db = 0; db < DP / 32; ++db)
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
-        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_cols<DP>(tile, row0 + 16 * s, 32 * db, lane), b[s], acc[db], 0, 0, 0);
+      for (int s = 0; s < 2; ++s) {
+        const bf16x8 a = read_cols<DP>(tile, row0 + 16 * s, 32 * db, lane);
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b[s], acc[db], 0, 0, 0);
+        if constexpr (TWO) (*acc2)[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b2[s], (*acc2)[db], 0, 0, 0);
+      }
   } else {
     const int half = lane >> 5, m = lane & 31;
 #pragma unroll
@@ -203,11 +213,14 @@ __device__ __forceinline__ void wait_and_meet() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-template <typename T, int DP>
+template <typename T, int DP, int SW>
 struct Ring {
-  static constexpr int CE = Elem<T>::CE, CH = DP / CE, TR = Elem<T>::TR, N = TR * CH / NT;   // N: loads of a wavefront per tile
-  static constexpr int BYTES = TR * DP * (int)sizeof(T);
+  static constexpr int CE = Elem<T>::CE, CH = DP / CE, TR = tile_rows<T, SW>(), N = TR * CH / NT;   // N: loads of a wavefront per tile
+  static constexpr int ELEMS = TR * DP, BYTES = ELEMS * (int)sizeof(T);
   static constexpr int STAGES = BYTES <= 8192 ? 3 : 2;      // 48 KB (64 KB) for pairs of tiles: three (two) workgroups to a compute unit
+  static constexpr int LDS = 2 * STAGES * BYTES;
+  // room for the join of the wavefronts' results: 128 rows of DP + 4 floats, and their statistics
+  static constexpr int JOIN_PITCH = DP + 4, JOIN = SW > 1 ? 128 * JOIN_PITCH * 4 + 128 * 12 : 0;
   static_assert(TR * CH % NT == 0, "chunks of a tile over the threads");
 };
 
@@ -248,9 +261,10 @@ __device__ __forceinline__ T* at(const void* base, const vf_attn_layout& l, int 
 }
 
 // This thread's chunks of one streamed tensor: where they lie for the tile that is loaded next.
-template <typename T, int DP>
+template <typename T, int DP, int SW>
 struct Source {
-  static constexpr int N = Ring<T, DP>::N, CH = Ring<T, DP>::CH, CE = Ring<T, DP>::CE, TR = Ring<T, DP>::TR;
+  static constexpr int N = Ring<T, DP, SW>::N, CH = Ring<T, DP, SW>::CH, WORDS = (Ring<T, DP, SW>::TR + 63) / 64;
+  static_assert(64 % (NT / CH) == 0, "rows of a load within one word of bits");
   const char* p[N];
   int g[N];                     // head among the group's (rows of several heads; else 0)
   // base: head 0 of row 0; rows r0, r0 + 1, ... are head r % group of row r / group
@@ -275,12 +289,14 @@ struct Source {
     return m;
   }
   // rows: bit r: row r of the tile is wanted; tile: LDS address of the tile's buffer for this wavefront
-  __device__ __forceinline__ void issue(uint64_t rows, uint32_t head, bool whole, const char* zeros, uint32_t tile) const {
-    const uint64_t mine = rows >> (threadIdx.x / CH);
+  __device__ __forceinline__ void issue(const uint64_t (&rows)[WORDS], uint32_t head, bool whole, const char* zeros, uint32_t tile) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const char* src = p[i];
-      if (!whole) src = ((mine >> (i * (NT / CH))) & (head >> i) & 1) ? p[i] : zeros;
+      if (!whole) {
+        const uint64_t mine = rows[i * (NT / CH) / 64] >> (threadIdx.x / CH);
+        src = ((mine >> (i * (NT / CH) % 64)) & (head >> i) & 1) ? p[i] : zeros;
+      }
       lds_load16(src, tile + i * (NT * 16));
     }
   }
@@ -356,17 +372,63 @@ __device__ __forceinline__ void store_row(T* row, const f32x16 (&acc)[DP / 32], 
     }
 }
 
+// a -= f b
+template <int N>
+__device__ __forceinline__ void remove(f32x16 (&a)[N], const f32x16 (&b)[N], float f) {
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) a[i][r] = fmaf(-f, b[i][r], a[i][r]);
+}
+// Row r of the problem in part w.part's partial results.
+__device__ __forceinline__ int64_t part_row(const AttnJob& j, const Problem& p, const Work& w, int r) {
+  return ((int64_t)w.part * j.s.batch * j.s.kv_heads + w.id) * p.rows + r;
+}
+// The sum over the SW wavefronts of `rows` (128 rows of fp32 in LDS, wavefront by wavefront), times factor[row], in order, to the
+// output's rows, or to the part's.
+template <typename T, int DP, int SW>
+__device__ __forceinline__ void join_waves(const AttnJob& j, const Problem& p, const Work& w, const AttnSplit& sp, const float* rows,
+                                           const float* factor, int r0, const void* base, const vf_attn_layout& l) {
+  constexpr int RW = 4 / SW, PITCH = Ring<T, DP, SW>::JOIN_PITCH;
+  const int dh = j.s.d_head;
+  for (int i = threadIdx.x; i < RW * WR * (DP / 4); i += NT) {
+    const int row = i / (DP / 4), e = i % (DP / 4) * 4, r = r0 + row;
+    if (r >= p.rows || e >= dh) continue;
+    float4 v = *reinterpret_cast<const float4*>(rows + row * PITCH + e);
+#pragma unroll
+    for (int k = 1; k < SW; ++k) {
+      const float4 x = *reinterpret_cast<const float4*>(rows + (k * RW * WR + row) * PITCH + e);
+      v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+    }
+    const float f = factor[row];
+    if (sp.parts > 1) {
+      *reinterpret_cast<float4*>(sp.out[0] + part_row(j, p, w, r) * dh + e) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
+      continue;
+    }
+    const RowOf ro = row_of(j, r);
+    T* out = at<T>(base, l, p.b, ro.t, p.hk * j.group + ro.g) + e;
+    if constexpr (sizeof(T) == 2) {
+      *reinterpret_cast<uint2*>(out) = make_uint2(f32x2_to_bf16x2(v.x * f, v.y * f), f32x2_to_bf16x2(v.z * f, v.w * f));
+    } else {
+      *reinterpret_cast<float4*>(out) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
+    }
+  }
+}
+
 // ---- forward ------------------------------------------------------------------------------------
-template <typename T, int DP>
-__global__ __launch_bounds__(NT, 2) void xattn_fwd_kernel(AttnJob j, AttnSplit sp) {
-  constexpr int TR = Elem<T>::TR, KB = TR / 32, ELEMS = Tile<T, DP>::ELEMS, STAGES = Ring<T, DP>::STAGES, BYTES = Ring<T, DP>::BYTES;
-  constexpr uint64_t ALL = TR == 64 ? ~0ull : (1ull << TR) - 1;
+template <typename T, int DP, int SW>
+__global__ __launch_bounds__(NT, DP * sizeof(T) <= 256 ? 2 : 1) void xattn_fwd_kernel(AttnJob j, AttnSplit sp) {
+  using R = Ring<T, DP, SW>;
+  constexpr int TR = R::TR, KB = TR / 32 / SW, RW = 4 / SW, ELEMS = R::ELEMS, STAGES = R::STAGES, BYTES = R::BYTES;
+  constexpr int WORDS = Source<T, DP, SW>::WORDS;
+  constexpr uint64_t ALL = TR >= 64 ? ~0ull : (1ull << TR) - 1, MINE = KB == 2 ? ~0ull : 0xffffffffull;
   extern __shared__ __attribute__((aligned(16))) char xattn_lds[];
   T* lds = reinterpret_cast<T*>(xattn_lds);                 // [STAGES][k, v][ELEMS]
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
   const Work w = work_of(sp);
   const Problem p = problem_of(j, w.id);
-  const int r = w.tile * (4 * WR) + wave * WR + (lane & 31);
+  const int block = __builtin_amdgcn_readfirstlane(wave) / RW * KB;       // first of this wavefront's blocks of a tile
+  const int r0 = w.tile * (RW * WR), r = r0 + wave % RW * WR + (lane & 31);
   const int kbeg = w.first * TR, kend = min(p.keys, kbeg + sp.per * TR);
   const bool mine = r < p.rows;
   const RowOf ro = row_of(j, mine ? r : 0);
@@ -382,14 +444,19 @@ __global__ __launch_bounds__(NT, 2) void xattn_fwd_kernel(AttnJob j, AttnSplit s
 
   const uint32_t lds0 = lds_address(lds) + __builtin_amdgcn_readfirstlane(wave) * 1024;
   const char* const zeros = zeros_address();
-  const uint32_t in_head = Source<T, DP>::head_bits(dh);
+  const uint32_t in_head = Source<T, DP, SW>::head_bits(dh);
   const int64_t kstep = TR * j.s.k.row * (int64_t)sizeof(T), vstep = TR * j.s.v.row * (int64_t)sizeof(T);
-  Source<T, DP> ks, vs;
+  Source<T, DP, SW> ks, vs;
   ks.init(j, at<const T>(j.k, j.s.k, p.b, 0, p.hk), j.s.k, kbeg, false);
   vs.init(j, at<const T>(j.v, j.s.v, p.b, 0, p.hk), j.s.v, kbeg, false);
   auto issue = [&](int k0, int buf) {                       // (behind the last tile: zeros, so that every tile counts alike)
-    const uint64_t vis = k0 < kend ? visible(j, p, k0) : 0;
-    const bool whole = dh == DP && (vis & ALL) == ALL;
+    uint64_t vis[WORDS], all = ~0ull;
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
+      vis[i] = k0 + 64 * i < kend ? visible(j, p, k0 + 64 * i) : 0;
+      all &= vis[i];
+    }
+    const bool whole = dh == DP && (all & ALL) == ALL;
     ks.issue(vis, in_head, whole, zeros, lds0 + buf * 2 * BYTES);
     vs.issue(vis, in_head, whole, zeros, lds0 + buf * 2 * BYTES + BYTES);
     ks.advance(kstep);
@@ -405,17 +472,17 @@ __global__ __launch_bounds__(NT, 2) void xattn_fwd_kernel(AttnJob j, AttnSplit s
   for (int k0 = kbeg; k0 < kend; k0 += TR, buf = (buf + 1) % STAGES) {
     const T* kt = lds + buf * 2 * ELEMS;
     const T* vt = kt + ELEMS;
-    wait_and_meet<(STAGES - 2) * 2 * Ring<T, DP>::N>();     // this tile is there, and nobody reads the one before it
+    wait_and_meet<(STAGES - 2) * 2 * R::N>();     // this tile is there, and nobody reads the one before it
     issue(k0 + (STAGES - 1) * TR, (buf + STAGES - 1) % STAGES);
-    const uint64_t now = visible(j, p, k0);
+    const uint64_t now = visible(j, p, k0 + 32 * block);
     f32x16 s[KB];
     if constexpr (KB == 2) {
-      dot_rows<T, DP, true>(s[0], kt, 0, q, s[1], kt, 32, q, lane);
+      dot_rows<T, DP, true>(s[0], kt, 32 * block, q, s[1], kt, 32 * block + 32, q, lane);
     } else {
       f32x16 none;
-      dot_rows<T, DP, false>(s[0], kt, 0, q, none, kt, 0, q, lane);
+      dot_rows<T, DP, false>(s[0], kt, 32 * block, q, none, kt, 0, q, lane);
     }
-    if ((now & ALL) != ALL) {
+    if ((now & MINE) != MINE) {
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
         const uint32_t bits = (uint32_t)(now >> (32 * kb)) >> (4 * half);
@@ -460,16 +527,50 @@ __global__ __launch_bounds__(NT, 2) void xattn_fwd_kernel(AttnJob j, AttnSplit s
         for (int i = 0; i < 16; ++i) o[db][i] *= fade;
     }
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) dot_cols<T, DP>(o, vt, 32 * kb, s[kb], lane);
+    for (int kb = 0; kb < KB; ++kb) dot_cols<T, DP>(o, vt, 32 * (block + kb), s[kb], lane);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // no load may find its LDS given away
-  if (!mine) return;
   l = pair_sum(l);
+  if constexpr (SW > 1) {
+    // the wavefronts' maxima and sums, then their results weighed by them
+    float* rows = reinterpret_cast<float*>(xattn_lds);
+    float* stat = rows + 128 * R::JOIN_PITCH;               // [128][maximum, sum], then [128] factors
+    const int slot = wave * WR + (lane & 31);
+    __syncthreads();                                        // nobody reads a tile any more
+    if (half == 0) *reinterpret_cast<float2*>(stat + 2 * slot) = make_float2(m, live ? l : 0.f);
+    __syncthreads();
+    float top = -INFINITY, total = 0.f;
+#pragma unroll
+    for (int k = 0; k < SW; ++k) {
+      const float2 x = *reinterpret_cast<const float2*>(stat + 2 * ((k * RW + wave % RW) * WR + (lane & 31)));
+      if (x.y != 0.f) top = fmaxf(top, x.x);
+    }
+    if (top == -INFINITY) top = 0.f;
+#pragma unroll
+    for (int k = 0; k < SW; ++k) {
+      const float2 x = *reinterpret_cast<const float2*>(stat + 2 * ((k * RW + wave % RW) * WR + (lane & 31)));
+      if (x.y != 0.f) total = fmaf(x.y, __builtin_amdgcn_exp2f((x.x - top) * c), total);
+    }
+    const float mine_w = live && l != 0.f ? __builtin_amdgcn_exp2f((m - top) * c) : 0.f;
+    const float factor = sp.parts > 1 ? 1.f : total != 0.f ? 1.f / total : 0.f;
+    store_row<float, DP>(rows + slot * R::JOIN_PITCH, o, mine_w, DP, half);
+    if (wave < RW && half == 0) {
+      stat[256 + slot] = factor;
+      if (mine) {
+        if (sp.parts > 1) *reinterpret_cast<float2*>(sp.stats + 2 * part_row(j, p, w, r)) = make_float2(top, total);
+        else if (j.lse) j.lse[((int64_t)p.b * j.s.q_heads + head) * j.s.q_rows + ro.t] = total != 0.f ? fmaf(top, j.s.scale, logf(total)) : -INFINITY;
+      }
+    }
+    __syncthreads();
+    join_waves<T, DP, SW>(j, p, w, sp, rows, stat + 256, r0, j.o, j.s.o);
+    return;
+  }
+  if (!mine) return;
   if (sp.parts > 1) {                                       // a part: unnormalised, with its maximum and sum
-    const int64_t row = ((int64_t)w.part * j.s.batch * j.s.kv_heads + w.id) * p.rows + r;
+    const int64_t row = part_row(j, p, w, r);
     if (!live) l = 0.f;
     if (half == 0) *reinterpret_cast<float2*>(sp.stats + 2 * row) = make_float2(m, l);
-    if (l != 0.f) store_row<float, DP>(sp.out[0] + row * dh, o, 1.f, dh, half);
+    store_row<float, DP>(sp.out[0] + row * dh, o, l != 0.f ? 1.f : 0.f, dh, half);
     return;
   }
   const bool any = live && l != 0.f;                        // (a NaN goes on)
@@ -479,16 +580,23 @@ __global__ __launch_bounds__(NT, 2) void xattn_fwd_kernel(AttnJob j, AttnSplit s
 }
 
 // ---- backward: dq, and lse / rowsum(dO o) of every row for the kernel behind it ---------------------
-template <typename T, int DP>
-__global__ __launch_bounds__(NT, DP * sizeof(T) <= 256 ? 2 : 1) void xattn_dq_kernel(AttnJob j, AttnSplit sp) {
-  constexpr int TR = Elem<T>::TR, KB = TR / 32, ELEMS = Tile<T, DP>::ELEMS, STAGES = Ring<T, DP>::STAGES, BYTES = Ring<T, DP>::BYTES;
-  constexpr uint64_t ALL = TR == 64 ? ~0ull : (1ull << TR) - 1;
+// rowsum(dO o) from the rounded o is off by e, and every dz by -p e: their sum, which should be 0, is -e.  The kernel behind is
+// given the exact rowsum.  Here dq is off by -scale e sum(p k): nothing beside the rounding of dz when many keys share a
+// row and o is small, but a third of the error at 77 keys (0.0027 of the norm, 0.0023 without it).  EXACT takes sum(p k) along and
+// removes it.
+template <typename T, int DP, int SW, bool EXACT>
+__global__ __launch_bounds__(NT, DP * sizeof(T) * (EXACT ? 2 : 1) <= 256 ? 2 : 1) void xattn_dq_kernel(AttnJob j, AttnSplit sp) {
+  using R = Ring<T, DP, SW>;
+  constexpr int TR = R::TR, KB = TR / 32 / SW, RW = 4 / SW, ELEMS = R::ELEMS, STAGES = R::STAGES, BYTES = R::BYTES;
+  constexpr int WORDS = Source<T, DP, SW>::WORDS;
+  constexpr uint64_t ALL = TR >= 64 ? ~0ull : (1ull << TR) - 1, MINE = KB == 2 ? ~0ull : 0xffffffffull;
   extern __shared__ __attribute__((aligned(16))) char xattn_lds[];
   T* lds = reinterpret_cast<T*>(xattn_lds);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
   const Work w = work_of(sp);
   const Problem p = problem_of(j, w.id);
-  const int r = w.tile * (4 * WR) + wave * WR + (lane & 31);
+  const int block = __builtin_amdgcn_readfirstlane(wave) / RW * KB;       // first of this wavefront's blocks of a tile
+  const int r0 = w.tile * (RW * WR), r = r0 + wave % RW * WR + (lane & 31);
   const int kbeg = w.first * TR, kend = min(p.keys, kbeg + sp.per * TR);
   const bool mine = r < p.rows;
   const RowOf ro = row_of(j, mine ? r : 0);
@@ -499,20 +607,26 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 256 ? 2 : 1) void xattn_dq_ke
   const bool live = lse_in != -INFINITY;                    // a row without a visible key has p = 0 everywhere
   const float lse = live ? lse_in * kLog2e : INFINITY;
 
-  f32x16 dq[DP / 32];
+  f32x16 dq[DP / 32], pk[EXACT ? DP / 32 : 1];
   clear(dq);
-  float rest = 0.f;                                         // sum of dz: 0 with the exact rowsum, here the error of o's rounding
+  clear(pk);
+  float rest = 0.f;                                         // sum of dz
 
   const uint32_t lds0 = lds_address(lds) + __builtin_amdgcn_readfirstlane(wave) * 1024;
   const char* const zeros = zeros_address();
-  const uint32_t in_head = Source<T, DP>::head_bits(dh);
+  const uint32_t in_head = Source<T, DP, SW>::head_bits(dh);
   const int64_t kstep = TR * j.s.k.row * (int64_t)sizeof(T), vstep = TR * j.s.v.row * (int64_t)sizeof(T);
-  Source<T, DP> ks, vs;
+  Source<T, DP, SW> ks, vs;
   ks.init(j, at<const T>(j.k, j.s.k, p.b, 0, p.hk), j.s.k, kbeg, false);
   vs.init(j, at<const T>(j.v, j.s.v, p.b, 0, p.hk), j.s.v, kbeg, false);
   auto issue = [&](int k0, int buf) {                       // (behind the last tile: zeros, so that every tile counts alike)
-    const uint64_t vis = k0 < kend ? visible(j, p, k0) : 0;
-    const bool whole = dh == DP && (vis & ALL) == ALL;
+    uint64_t vis[WORDS], all = ~0ull;
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
+      vis[i] = k0 + 64 * i < kend ? visible(j, p, k0 + 64 * i) : 0;
+      all &= vis[i];
+    }
+    const bool whole = dh == DP && (all & ALL) == ALL;
     ks.issue(vis, in_head, whole, zeros, lds0 + buf * 2 * BYTES);
     vs.issue(vis, in_head, whole, zeros, lds0 + buf * 2 * BYTES + BYTES);
     ks.advance(kstep);
@@ -548,34 +662,59 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 256 ? 2 : 1) void xattn_dq_ke
   for (int k0 = kbeg; k0 < kend; k0 += TR, buf = (buf + 1) % STAGES) {
     const T* kt = lds + buf * 2 * ELEMS;
     const T* vt = kt + ELEMS;
-    wait_and_meet<(STAGES - 2) * 2 * Ring<T, DP>::N>();     // this tile is there, and nobody reads the one before it
+    wait_and_meet<(STAGES - 2) * 2 * R::N>();     // this tile is there, and nobody reads the one before it
     issue(k0 + (STAGES - 1) * TR, (buf + STAGES - 1) % STAGES);
-    const uint64_t now = visible(j, p, k0);
+    const uint64_t now = visible(j, p, k0 + 32 * block);
 #pragma unroll 1
     for (int kb = 0; kb < KB; ++kb) {
-      f32x16 s[1], dp[1];
-      dot_rows<T, DP, true, 2>(s[0], kt, 32 * kb, q, dp[0], vt, 32 * kb, g, lane);
-      const uint32_t bits = (uint32_t)(now >> (32 * kb)) >> (4 * half);
+      const uint32_t seen = (uint32_t)(now >> (32 * kb)), bits = seen >> (4 * half);
+      if (seen == 0) continue;                              // (the same for the whole wavefront)
+      f32x16 s, dp, pr;
+      dot_rows<T, DP, true, 2>(s, kt, 32 * (block + kb), q, dp, vt, 32 * (block + kb), g, lane);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        float pr = __builtin_amdgcn_exp2f(fminf(fmaf(s[0][i], c, -lse), 0.f));   // (scores so far out that the rounding of lse passes 1)
-        if (!((bits >> acc_row(i, 0)) & 1)) pr = 0.f;
-        s[0][i] = pr * (dp[0][i] - delta);
-        rest += s[0][i];
+        float x = __builtin_amdgcn_exp2f(fminf(fmaf(s[i], c, -lse), 0.f));   // (scores so far out that the rounding of lse passes 1)
+        if (!((bits >> acc_row(i, 0)) & 1)) x = 0.f;
+        pr[i] = x;
+        s[i] = x * (dp[i] - delta);
+        rest += s[i];
       }
-      dot_cols<T, DP>(dq, kt, 32 * kb, s[0], lane);
+      if constexpr (EXACT) dot_cols<T, DP, true>(dq, kt, 32 * (block + kb), s, lane, &pk, &pr);
+      else dot_cols<T, DP>(dq, kt, 32 * (block + kb), s, lane);
     }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  if (!mine) return;
   rest = pair_sum(rest);
+  if constexpr (SW > 1) {
+    float* rows = reinterpret_cast<float*>(xattn_lds);
+    float* stat = rows + 128 * R::JOIN_PITCH;               // [128] rests, [128] factors
+    const int slot = wave * WR + (lane & 31);
+    __syncthreads();
+    if (half == 0) { stat[slot] = rest; stat[256 + slot] = sp.parts > 1 ? 1.f : j.s.scale; }
+    __syncthreads();
+    rest = 0.f;
+#pragma unroll
+    for (int k = 0; k < SW; ++k) rest += stat[(k * RW + wave % RW) * WR + (lane & 31)];
+    if constexpr (EXACT) remove(dq, pk, rest);
+    store_row<float, DP>(rows + slot * R::JOIN_PITCH, dq, 1.f, DP, half);
+    __syncthreads();
+    if (wave < RW && half == 0 && mine) {
+      if (sp.parts > 1) *reinterpret_cast<float2*>(sp.stats + 2 * part_row(j, p, w, r)) = make_float2(rest, delta);
+      else j.row_delta[(int64_t)w.id * p.rows + r] = delta + rest;
+      if (w.part == 0) j.row_lse[(int64_t)w.id * p.rows + r] = lse;
+    }
+    join_waves<T, DP, SW>(j, p, w, sp, rows, stat + 256, r0, j.dq, j.s.dq);
+    return;
+  }
+  if (!mine) return;
   if (sp.parts > 1) {
-    const int64_t row = ((int64_t)w.part * j.s.batch * j.s.kv_heads + w.id) * p.rows + r;
+    const int64_t row = part_row(j, p, w, r);
     if (half == 0) *reinterpret_cast<float2*>(sp.stats + 2 * row) = make_float2(rest, delta);
     store_row<float, DP>(sp.out[0] + row * dh, dq, 1.f, dh, half);
     if (w.part == 0 && half == 0) j.row_lse[(int64_t)w.id * p.rows + r] = lse;
     return;
   }
+  if constexpr (EXACT) remove(dq, pk, rest);
   if (half == 0) {
     j.row_lse[(int64_t)w.id * p.rows + r] = lse;
     j.row_delta[(int64_t)w.id * p.rows + r] = delta + rest;
@@ -586,8 +725,9 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 256 ? 2 : 1) void xattn_dq_ke
 // ---- backward: dk and dv ------------------------------------------------------------------------------
 template <typename T, int DP>
 __global__ __launch_bounds__(NT, DP * sizeof(T) <= 128 ? 2 : 1) void xattn_dkv_kernel(AttnJob j, AttnSplit sp) {
-  constexpr int TR = Elem<T>::TR, QB = TR / 32, ELEMS = Tile<T, DP>::ELEMS, STAGES = Ring<T, DP>::STAGES, BYTES = Ring<T, DP>::BYTES;
-  constexpr uint64_t ALL = TR == 64 ? ~0ull : (1ull << TR) - 1;
+  using R = Ring<T, DP, 1>;
+  constexpr int TR = R::TR, QB = TR / 32, ELEMS = R::ELEMS, STAGES = R::STAGES, BYTES = R::BYTES;
+  constexpr uint64_t ALL = TR >= 64 ? ~0ull : (1ull << TR) - 1;
   extern __shared__ __attribute__((aligned(16))) char xattn_lds[];
   T* lds = reinterpret_cast<T*>(xattn_lds);                 // [STAGES][q, dO][ELEMS], then [STAGES][lse, delta][64]
   float* stats = reinterpret_cast<float*>(lds + 2 * STAGES * ELEMS);
@@ -611,16 +751,16 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 128 ? 2 : 1) void xattn_dkv_k
   const char* const zeros = zeros_address();
   const int beg = w.first * TR, stop = min(rows, beg + sp.per * TR);
   const int end = w.tile * (4 * WR) < p.keys ? stop : beg;  // (a tile without a visible key: nothing but zeros to write)
-  const uint32_t in_head = Source<T, DP>::head_bits(dh);
+  const uint32_t in_head = Source<T, DP, 1>::head_bits(dh);
   const int step_t = TR / j.group, step_g = TR % j.group;
   const int64_t qstep = (step_t * j.s.q.row + step_g * j.s.q.head) * (int64_t)sizeof(T), qover = (j.s.q.row - j.group * j.s.q.head) * (int64_t)sizeof(T);
   const int64_t gstep = (step_t * j.s.d_o.row + step_g * j.s.d_o.head) * (int64_t)sizeof(T), gover = (j.s.d_o.row - j.group * j.s.d_o.head) * (int64_t)sizeof(T);
-  Source<T, DP> qs, gs;
+  Source<T, DP, 1> qs, gs;
   qs.init(j, at<const T>(j.q, j.s.q, p.b, 0, p.hk * j.group), j.s.q, beg, true);
   gs.init(j, at<const T>(j.d_o, j.s.d_o, p.b, 0, p.hk * j.group), j.s.d_o, beg, true);
   auto issue = [&](int r0, int buf) {
-    const uint64_t want = first_bits(stop - r0);
-    const bool whole = dh == DP && (want & ALL) == ALL;
+    const uint64_t want[1] = {first_bits(stop - r0)};
+    const bool whole = dh == DP && (want[0] & ALL) == ALL;
     qs.issue(want, in_head, whole, zeros, lds0 + buf * 2 * BYTES);
     gs.issue(want, in_head, whole, zeros, lds0 + buf * 2 * BYTES + BYTES);
     if (step_g == 0) {
@@ -649,10 +789,12 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 128 ? 2 : 1) void xattn_dkv_k
     const T* qt = lds + buf * 2 * ELEMS;
     const T* gt = qt + ELEMS;
     const float* st = stats + buf * 128;
-    wait_and_meet<(STAGES - 2) * (2 * Ring<T, DP>::N + 2)>();
+    wait_and_meet<(STAGES - 2) * (2 * R::N + 2)>();
     issue(r0 + (STAGES - 1) * TR, (buf + STAGES - 1) % STAGES);
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
+      if (DP <= 64 && r0 + 32 * qb >= stop) break;          // (behind the last row, the same for the whole workgroup; two blocks in one
+                                                            // piece of code are worth more at 128: 650 us, with the break 720)
       f32x16 s[1], dp[1];
       dot_rows<T, DP, true>(s[0], qt, 32 * qb, k, dp[0], gt, 32 * qb, v, lane);
 #pragma unroll
@@ -698,6 +840,7 @@ __device__ __forceinline__ void join_rows(const AttnJob& j, const AttnSplit& sp,
   float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
   float top = -INFINITY, total = 0.f, delta = 0.f, factor = 1.f;
   if constexpr (KIND == 0) {
+#pragma unroll 4
     for (int k = 0; k < sp.parts; ++k) {
       const float2 ml = *reinterpret_cast<const float2*>(sp.stats + 2 * (i + k * step));
       if (ml.y != 0.f) top = fmaxf(top, ml.x);
@@ -705,23 +848,21 @@ __device__ __forceinline__ void join_rows(const AttnJob& j, const AttnSplit& sp,
     if (top == -INFINITY) top = 0.f;
   }
   const float c = j.s.scale * kLog2e;
-  for (int k = 0; k < sp.parts; ++k) {
+#pragma unroll 4
+  for (int k = 0; k < sp.parts; ++k) {                      // (four parts' loads under way together)
     float w = 1.f;
     if constexpr (KIND < 2) {
       const float2 st = *reinterpret_cast<const float2*>(sp.stats + 2 * (i + k * step));
       if constexpr (KIND == 0) {
-        if (st.y == 0.f) continue;                          // (its rows were not written)
-        w = __builtin_amdgcn_exp2f((st.x - top) * c);
+        w = st.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((st.x - top) * c);
         total = fmaf(st.y, w, total);
       } else {
         if (k == 0) delta = st.y;
         total += st.x;
       }
     }
-    if (e < dh) {
-      const float4 v = *reinterpret_cast<const float4*>(part + k * step * dh);
-      sum.x = fmaf(v.x, w, sum.x); sum.y = fmaf(v.y, w, sum.y); sum.z = fmaf(v.z, w, sum.z); sum.w = fmaf(v.w, w, sum.w);
-    }
+    const float4 v = e < dh ? *reinterpret_cast<const float4*>(part + k * step * dh) : make_float4(0.f, 0.f, 0.f, 0.f);
+    sum.x = fmaf(v.x, w, sum.x); sum.y = fmaf(v.y, w, sum.y); sum.z = fmaf(v.z, w, sum.z); sum.w = fmaf(v.w, w, sum.w);
   }
   T* out;
   if constexpr (KIND < 2) {
@@ -761,15 +902,20 @@ __global__ __launch_bounds__(NT) void xattn_join_kernel(AttnJob j, AttnSplit sp,
   }
 }
 
-// How the streamed side is split: one part per tile of held rows where those fill the compute units or the streamed tiles are few;
-// else as many parts as give every unit two workgroups.  Joining costs a launch and a pass over fp32 partial results, about 8 us,
-// a streamed tile 1.2 us (bf16) or 2.5 (fp32): fewer than 8 (4) tiles saved do not pay (192 workgroups of 7 tiles,
-// three parts: 12.6 us of forward became 11.8 + 8.4).
-constexpr int kUnits = 256, kMaxParts = 64;
-AttnSplit split_of(int64_t problems, int held, int streamed, int tile_rows) {
-  const int least_saved = tile_rows == 64 ? 8 : 4;
+// How the streamed side is split.  First among the wavefronts of a workgroup (sw): with 32 held rows to a workgroup instead of 128
+// there are four times as many workgroups and each goes through a quarter of the tiles' blocks, as long as that leaves at most
+// kFew workgroups.  Then into parts: one where the workgroups fill the compute units or the streamed tiles are few; else as
+// many as give every unit two workgroups.  Joining the parts costs a launch and a pass over fp32 partial results, about
+// 8 us, a streamed tile 1.2 us (bf16) or 2.5 (fp32): fewer than 8 (4) tiles saved do not pay.
+constexpr int kUnits = 256, kMaxParts = 64, kFew = 512;
+AttnSplit split_of(int64_t problems, int held, int streamed, int tile_rows, int most_sw, bool wide_tile) {
   AttnSplit sp{};
-  sp.tiles = (held + 4 * WR - 1) / (4 * WR);
+  sp.sw = 1;
+  for (int sw = 2; sw <= most_sw; sw *= 2)
+    if (problems * ((held + 128 / sw - 1) / (128 / sw)) <= kFew) sp.sw = sw;
+  const int block = 128 / sp.sw, least_saved = wide_tile ? 8 : 4;
+  tile_rows = std::max(tile_rows, 32 * sp.sw);
+  sp.tiles = (held + block - 1) / block;
   const int all = std::max(1, (streamed + tile_rows - 1) / tile_rows);
   const int64_t groups = problems * sp.tiles;
   sp.per = all;
@@ -781,13 +927,16 @@ AttnSplit split_of(int64_t problems, int held, int streamed, int tile_rows) {
   sp.parts = (all + sp.per - 1) / sp.per;
   return sp;
 }
-int tile_rows_of(const vf_attn_shape& s) { return s.dtype == VF_BF16 ? Elem<bf16_t>::TR : Elem<float>::TR; }
-// The splits of the forward and dq kernels, and of the dk/dv kernel.
+// The splits of the forward and dq kernels, and of the dk/dv kernel.  (fp32 heads of more than 64 elements: tiles for four wavefronts
+// would not fit the LDS.)
 AttnSplit split_rows(const vf_attn_shape& s) {
-  return split_of((int64_t)s.batch * s.kv_heads, s.q_heads / s.kv_heads * s.q_rows, s.k_rows, tile_rows_of(s));
+  const bool b = s.dtype == VF_BF16;
+  return split_of((int64_t)s.batch * s.kv_heads, s.q_heads / s.kv_heads * s.q_rows, s.k_rows, b ? Elem<bf16_t>::TR : Elem<float>::TR,
+                  b || s.d_head <= 64 ? 4 : 2, b);
 }
 AttnSplit split_keys(const vf_attn_shape& s) {
-  return split_of((int64_t)s.batch * s.kv_heads, s.k_rows, s.q_heads / s.kv_heads * s.q_rows, tile_rows_of(s));
+  const bool b = s.dtype == VF_BF16;
+  return split_of((int64_t)s.batch * s.kv_heads, s.k_rows, s.q_heads / s.kv_heads * s.q_rows, b ? Elem<bf16_t>::TR : Elem<float>::TR, 1, b);
 }
 int64_t round4(int64_t floats) { return (floats + 3) & ~int64_t(3); }
 // Floats of the parts of a pass over the rows (results and two statistics a row), and over the keys (dk and dv).
@@ -816,45 +965,69 @@ int launch_join(const AttnJob& j, const AttnSplit& sp, int64_t rows, hipStream_t
   return VF_OK;
 }
 
-template <typename T, int DP>
-int launch_fwd(const AttnJob& j, float* ws, hipStream_t st) {
-  constexpr int lds = 2 * Ring<T, DP>::STAGES * Ring<T, DP>::BYTES;
+template <typename T, int DP, int SW>
+int launch_fwd(const AttnJob& j, const AttnSplit& sp, hipStream_t st) {
+  constexpr int lds = std::max(Ring<T, DP, SW>::LDS, Ring<T, DP, SW>::JOIN);
   static std::atomic<uint64_t> ready{0};
-  VF_TRY(allow_lds(reinterpret_cast<const void*>(&xattn_fwd_kernel<T, DP>), lds, ready));
+  VF_TRY(allow_lds(reinterpret_cast<const void*>(&xattn_fwd_kernel<T, DP, SW>), lds, ready));
+  xattn_fwd_kernel<T, DP, SW><<<dim3(j.s.batch * j.s.kv_heads, sp.tiles, sp.parts), NT, lds, st>>>(j, sp);
+  VF_LAUNCH_CHECK();
+  return VF_OK;
+}
+constexpr int kExactKeys = 512;
+template <typename T, int DP, int SW, bool EXACT>
+int launch_dq_of(const AttnJob& j, const AttnSplit& sp, hipStream_t st) {
+  constexpr int lds = std::max(Ring<T, DP, SW>::LDS, Ring<T, DP, SW>::JOIN);
+  static std::atomic<uint64_t> ready{0};
+  VF_TRY(allow_lds(reinterpret_cast<const void*>(&xattn_dq_kernel<T, DP, SW, EXACT>), lds, ready));
+  xattn_dq_kernel<T, DP, SW, EXACT><<<dim3(j.s.batch * j.s.kv_heads, sp.tiles, sp.parts), NT, lds, st>>>(j, sp);
+  VF_LAUNCH_CHECK();
+  return VF_OK;
+}
+template <typename T, int DP, int SW>
+int launch_dq(const AttnJob& j, const AttnSplit& sp, hipStream_t st) {
+  // (parts are made of more keys than that)
+  if constexpr (sizeof(T) == 2) return j.s.k_rows <= kExactKeys ? launch_dq_of<T, DP, SW, true>(j, sp, st) : launch_dq_of<T, DP, SW, false>(j, sp, st);
+  else return launch_dq_of<T, DP, SW, false>(j, sp, st);
+}
+template <typename T, int DP>
+int launch_dkv(const AttnJob& j, const AttnSplit& sp, hipStream_t st) {
+  constexpr int lds = Ring<T, DP, 1>::LDS + Ring<T, DP, 1>::STAGES * 512;
+  static std::atomic<uint64_t> ready{0};
+  VF_TRY(allow_lds(reinterpret_cast<const void*>(&xattn_dkv_kernel<T, DP>), lds, ready));
+  xattn_dkv_kernel<T, DP><<<dim3(j.s.batch * j.s.kv_heads, sp.tiles, sp.parts), NT, lds, st>>>(j, sp);
+  VF_LAUNCH_CHECK();
+  return VF_OK;
+}
+
+// The passes over the rows (forward, dq) and over the keys, with their joins.
+template <typename T, int DP>
+int pass_rows(const AttnJob& j, float* ws, bool backward, hipStream_t st) {
   const int64_t rows = (int64_t)j.s.batch * j.s.q_heads * j.s.q_rows;
   AttnSplit sp = split_rows(j.s);
   sp.out[0] = ws;
   sp.stats = ws + sp.parts * rows * j.s.d_head;
-  xattn_fwd_kernel<T, DP><<<dim3(j.s.batch * j.s.kv_heads, sp.tiles, sp.parts), NT, lds, st>>>(j, sp);
-  VF_LAUNCH_CHECK();
-  return sp.parts > 1 ? launch_join<T, 0>(j, sp, rows, st) : VF_OK;
+  if constexpr (sizeof(T) == 2 || DP <= 64) {
+    if (sp.sw == 4) VF_TRY((backward ? launch_dq<T, DP, 4>(j, sp, st) : launch_fwd<T, DP, 4>(j, sp, st)));
+  }
+  if (sp.sw == 2) VF_TRY((backward ? launch_dq<T, DP, 2>(j, sp, st) : launch_fwd<T, DP, 2>(j, sp, st)));
+  if (sp.sw == 1) VF_TRY((backward ? launch_dq<T, DP, 1>(j, sp, st) : launch_fwd<T, DP, 1>(j, sp, st)));
+  if (sp.parts == 1) return VF_OK;
+  return backward ? launch_join<T, 1>(j, sp, rows, st) : launch_join<T, 0>(j, sp, rows, st);
 }
-
+template <typename T, int DP>
+int pass_keys(const AttnJob& j, float* ws, hipStream_t st) {
+  const int64_t rows = (int64_t)j.s.batch * j.s.kv_heads * j.s.k_rows;
+  AttnSplit sp = split_keys(j.s);
+  sp.out[0] = ws;
+  sp.out[1] = ws + sp.parts * rows * j.s.d_head;
+  VF_TRY((launch_dkv<T, DP>(j, sp, st)));
+  return sp.parts > 1 ? launch_join<T, 2>(j, sp, rows, st) : VF_OK;
+}
 template <typename T, int DP>
 int launch_bwd(const AttnJob& j, float* ws, hipStream_t st) {
-  constexpr int lds = 2 * Ring<T, DP>::STAGES * Ring<T, DP>::BYTES, lds_kv = lds + Ring<T, DP>::STAGES * 512;
-  static std::atomic<uint64_t> ready_q{0}, ready_kv{0};
-  VF_TRY(allow_lds(reinterpret_cast<const void*>(&xattn_dq_kernel<T, DP>), lds, ready_q));
-  VF_TRY(allow_lds(reinterpret_cast<const void*>(&xattn_dkv_kernel<T, DP>), lds_kv, ready_kv));
-  const int problems = j.s.batch * j.s.kv_heads;
-  if (j.s.q_rows) {
-    const int64_t rows = (int64_t)j.s.batch * j.s.q_heads * j.s.q_rows;
-    AttnSplit sp = split_rows(j.s);
-    sp.out[0] = ws;
-    sp.stats = ws + sp.parts * rows * j.s.d_head;
-    xattn_dq_kernel<T, DP><<<dim3(problems, sp.tiles, sp.parts), NT, lds, st>>>(j, sp);
-    VF_LAUNCH_CHECK();
-    if (sp.parts > 1) VF_TRY((launch_join<T, 1>(j, sp, rows, st)));
-  }
-  if (j.s.k_rows) {
-    const int64_t rows = (int64_t)problems * j.s.k_rows;
-    AttnSplit sp = split_keys(j.s);                         // (its parts take the place of the rows' ones)
-    sp.out[0] = ws;
-    sp.out[1] = ws + sp.parts * rows * j.s.d_head;
-    xattn_dkv_kernel<T, DP><<<dim3(problems, sp.tiles, sp.parts), NT, lds_kv, st>>>(j, sp);
-    VF_LAUNCH_CHECK();
-    if (sp.parts > 1) VF_TRY((launch_join<T, 2>(j, sp, rows, st)));
-  }
+  if (j.s.q_rows) VF_TRY((pass_rows<T, DP>(j, ws, true, st)));
+  if (j.s.k_rows) VF_TRY((pass_keys<T, DP>(j, ws, st)));     // (its parts take the place of the rows' ones)
   return VF_OK;
 }
 
@@ -887,8 +1060,8 @@ int launch_attn(AttnJob j, void* workspace, hipStream_t st) {
   VF_TRY(make_bits(j, ws, st));
   ws += mask_floats(j.s);
   const bool wide = j.s.d_head > 64;
-  if (j.s.dtype == VF_BF16) return wide ? launch_fwd<bf16_t, 128>(j, ws, st) : launch_fwd<bf16_t, 64>(j, ws, st);
-  return wide ? launch_fwd<float, 128>(j, ws, st) : launch_fwd<float, 64>(j, ws, st);
+  if (j.s.dtype == VF_BF16) return wide ? pass_rows<bf16_t, 128>(j, ws, false, st) : pass_rows<bf16_t, 64>(j, ws, false, st);
+  return wide ? pass_rows<float, 128>(j, ws, false, st) : pass_rows<float, 64>(j, ws, false, st);
 }
 
 int launch_attn_bwd(AttnJob j, void* workspace, hipStream_t st) {

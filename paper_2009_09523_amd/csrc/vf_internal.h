@@ -583,10 +583,10 @@ struct AttnJob {
   const uint64_t* bits; int words;                       // key_mask as bits, `words` words a sample, or null
   float *row_lse, *row_delta;                            // backward: log2-domain lse and rowsum(dO o) of every row, in row order
 };
-// How a kernel's workgroups share the work: `tiles` tiles of held rows, the streamed side in `parts` parts of `per` tiles,
-// whose partial results go to out (and stats) and are joined by a kernel behind it.
+// How a kernel's workgroups share the work: `tiles` tiles of held rows (128 / sw), the streamed side among `sw` wavefronts and in
+// `parts` parts of `per` tiles, whose partial results go to out (and stats) and are joined by a kernel behind it.
 struct AttnSplit {
-  int tiles, parts, per;
+  int sw, tiles, parts, per;
   float* out[2];
   float* stats;
 };
