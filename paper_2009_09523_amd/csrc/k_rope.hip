@@ -241,6 +241,8 @@ __global__ __launch_bounds__(NT) void rope_kernel(RopeJob j, Turns turns) {
   }
 }
 
+template <int C> __host__ __device__ __forceinline__ int unit_pitch(int dh) { return C > 1 ? dh + 4 : dh + 1; }
+
 // Backward pass of the norm with rotation.  A workgroup walks row tiles blockIdx.x, blockIdx.x + gridDim.x, ... so that the
 // partial sums of dgamma stay few; they are added in the order of the workgroups by gamma_finish_kernel.
 template <typename T, int C, int NS>
@@ -323,15 +325,24 @@ __global__ __launch_bounds__(NT) void norm_bwd_kernel(RopeJob j, Turns turns) {
   if (!j.partial) return;
   // The units' sums side by side in LDS; then 256 threads take the columns, several groups of units to a column where there are
   // fewer than 256, each group in the order of its units, and the groups in theirs.
+  // (Rows of the units four banks apart: at a pitch of 64 the 16 units of a wavefront met on the same banks, 3 us of 11.)
   float* sums = reinterpret_cast<float*>(rope_cs);
+  const int pitch = unit_pitch<C>(j.dh);
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < NS; ++i)
+  for (int i = 0; i < NS; ++i) {
+    float* mine = sums + unit * pitch;
+    if constexpr (C > 1) {
 #pragma unroll
-    for (int e = 0; e < C; ++e) {
-      if (k[i].a0 >= 0) sums[unit * j.dh + k[i].a0 + e] = s0[i][e];
-      if (k[i].a1 >= 0) sums[unit * j.dh + k[i].a1 + e] = s1[i][e];
+      for (int e = 0; e < C; e += 4) {
+        if (k[i].a0 >= 0) *reinterpret_cast<float4*>(mine + k[i].a0 + e) = make_float4(s0[i][e], s0[i][e + 1], s0[i][e + 2], s0[i][e + 3]);
+        if (k[i].a1 >= 0) *reinterpret_cast<float4*>(mine + k[i].a1 + e) = make_float4(s1[i][e], s1[i][e + 1], s1[i][e + 2], s1[i][e + 3]);
+      }
+    } else {
+      if (k[i].a0 >= 0) mine[k[i].a0] = s0[i][0];
+      if (k[i].a1 >= 0) mine[k[i].a1] = s1[i][0];
     }
+  }
   __syncthreads();
   float* out = j.partial + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * j.dh;
   const int groups = max(1, min(units, NT / j.dh)), per = (units + groups - 1) / groups;
@@ -341,7 +352,7 @@ __global__ __launch_bounds__(NT) void norm_bwd_kernel(RopeJob j, Turns turns) {
     if (c < j.dh && g < groups) {
       const int first = g * per, last = min(units, first + per);
 #pragma unroll 8
-      for (int u = first; u < last; ++u) v += sums[u * j.dh + c];
+      for (int u = first; u < last; ++u) v += sums[u * pitch + c];
     }
     if (groups > 1) {                                      // (then c0 is 0: one turn)
       __syncthreads();
@@ -440,7 +451,7 @@ Plan plan_of(RopeJob& j, int C, bool bwd) {
   const int64_t gx = std::min((j.rows + j.tile - 1) / j.tile, bwd ? kMaxPartials : kMaxRowGroups);
   p.grid = dim3((unsigned)gx, (unsigned)(j.q_blocks + k_blocks));
   p.lds = (size_t)j.tile * (j.rot / 2) * sizeof(float2);
-  if (bwd) p.lds = std::max(p.lds, (size_t)units * j.dh * sizeof(float));
+  if (bwd) p.lds = std::max(p.lds, (size_t)units * (C > 1 ? unit_pitch<4>(j.dh) : unit_pitch<1>(j.dh)) * sizeof(float));
   return p;
 }
 

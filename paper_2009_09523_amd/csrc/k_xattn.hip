@@ -324,16 +324,37 @@ __device__ __forceinline__ const char* zeros_address() {
   return z;
 }
 
-// Which of the keys k0 .. k0 + 63 (k0 a multiple of 32) are visible, one bit each.  A mask comes as such bits (mask_bits_kernel),
-// read by scalar loads, which do not stand in the queue of the tiles' loads.
-__device__ __forceinline__ uint64_t visible(const AttnJob& j, const Problem& p, int k0) {
+// Which of the keys k0 .. k0 + 63 are visible, one bit each.  A mask comes as such bits.  Up to kMaskWords words a workgroup makes
+// them itself from the part of the mask it needs (take_mask: words[i], keys first + 64 i ...); longer ones come from
+// mask_bits_kernel (k0 a multiple of 32) by scalar loads, which do not stand in the queue of the tiles' loads.
+constexpr int kMaskWords = 64;
+struct Mask { uint64_t* words; int first; };
+__device__ __forceinline__ uint64_t visible(const AttnJob& j, const Problem& p, const Mask& m, int k0) {
   const int n = p.keys - k0;
   uint64_t bits = first_bits(n);
-  if (j.bits && n > 0) {
-    const __attribute__((address_space(4))) uint64_t* w = (const __attribute__((address_space(4))) uint64_t*)(j.bits + (int64_t)p.b * j.words + (k0 >> 6));
-    bits &= w[0] >> (k0 & 32);
+  if (j.key_mask && n > 0) {
+    if (j.bits) {
+      const __attribute__((address_space(4))) uint64_t* w = (const __attribute__((address_space(4))) uint64_t*)(j.bits + (int64_t)p.b * j.words + (k0 >> 6));
+      bits &= w[0] >> (k0 & 32);
+    } else {
+      const uint64_t w = m.words[(k0 - m.first) >> 6] >> ((k0 - m.first) & 32);
+      bits &= (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)w) | (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(w >> 32)) << 32;
+    }
   }
   return bits;
+}
+__device__ __forceinline__ Mask take_mask(const AttnJob& j, const Problem& p, char* lds, int beg, int end) {
+  const Mask m{reinterpret_cast<uint64_t*>(lds), beg};
+  if (j.key_mask && !j.bits && beg < end) {
+    const int lane = threadIdx.x & 63;
+    for (int i = threadIdx.x >> 6; beg + 64 * i < end; i += NT / 64) {
+      const int k = beg + 64 * i + lane;
+      const uint64_t on = __ballot(k < end && j.key_mask[(int64_t)p.b * j.s.k_rows + k] != 0);
+      if (lane == 0) m.words[i] = on;
+    }
+    __syncthreads();
+  }
+  return m;
 }
 // bits[b][w], bit i: key 64 w + i of the mask is visible.
 __global__ __launch_bounds__(NT) void mask_bits_kernel(const uint8_t* __restrict__ mask, int keys, int words, int64_t n, uint64_t* __restrict__ bits) {
@@ -384,35 +405,38 @@ __device__ __forceinline__ void remove(f32x16 (&a)[N], const f32x16 (&b)[N], flo
 __device__ __forceinline__ int64_t part_row(const AttnJob& j, const Problem& p, const Work& w, int r) {
   return ((int64_t)w.part * j.s.batch * j.s.kv_heads + w.id) * p.rows + r;
 }
-// The sum over the SW wavefronts of `rows` (128 rows of fp32 in LDS, wavefront by wavefront), times factor[row], in order, to the
-// output's rows, or to the part's.
-template <typename T, int DP, int SW>
-__device__ __forceinline__ void join_waves(const AttnJob& j, const Problem& p, const Work& w, const AttnSplit& sp, const float* rows,
-                                           const float* factor, int r0, const void* base, const vf_attn_layout& l) {
+// The sum over the SW wavefronts of `rows` (128 rows of fp32 in LDS, wavefront by wavefront) in order, times factor(row): held
+// row r0 + row, below `end`, goes to out(r), or, of a part, to part + r d_head.
+template <typename T, int DP, int SW, typename F, typename O>
+__device__ __forceinline__ void join_waves(const float* rows, F factor, int r0, int end, int dh, float* part, O out) {
   constexpr int RW = 4 / SW, PITCH = Ring<T, DP, SW>::JOIN_PITCH;
-  const int dh = j.s.d_head;
   for (int i = threadIdx.x; i < RW * WR * (DP / 4); i += NT) {
     const int row = i / (DP / 4), e = i % (DP / 4) * 4, r = r0 + row;
-    if (r >= p.rows || e >= dh) continue;
+    if (r >= end || e >= dh) continue;
     float4 v = *reinterpret_cast<const float4*>(rows + row * PITCH + e);
 #pragma unroll
     for (int k = 1; k < SW; ++k) {
       const float4 x = *reinterpret_cast<const float4*>(rows + (k * RW * WR + row) * PITCH + e);
       v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
     }
-    const float f = factor[row];
-    if (sp.parts > 1) {
-      *reinterpret_cast<float4*>(sp.out[0] + part_row(j, p, w, r) * dh + e) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
-      continue;
-    }
-    const RowOf ro = row_of(j, r);
-    T* out = at<T>(base, l, p.b, ro.t, p.hk * j.group + ro.g) + e;
-    if constexpr (sizeof(T) == 2) {
-      *reinterpret_cast<uint2*>(out) = make_uint2(f32x2_to_bf16x2(v.x * f, v.y * f), f32x2_to_bf16x2(v.z * f, v.w * f));
+    const float f = factor(row);
+    if (part) {
+      *reinterpret_cast<float4*>(part + (int64_t)r * dh + e) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
+    } else if constexpr (sizeof(T) == 2) {
+      *reinterpret_cast<uint2*>(out(r) + e) = make_uint2(f32x2_to_bf16x2(v.x * f, v.y * f), f32x2_to_bf16x2(v.z * f, v.w * f));
     } else {
-      *reinterpret_cast<float4*>(out) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
+      *reinterpret_cast<float4*>(out(r) + e) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
     }
   }
+}
+// The same for rows of queries.
+template <typename T, int DP, int SW, typename F>
+__device__ __forceinline__ void join_queries(const AttnJob& j, const Problem& p, const Work& w, const AttnSplit& sp, const float* rows, F factor,
+                                             int r0, const void* base, const vf_attn_layout& l) {
+  join_waves<T, DP, SW>(rows, factor, r0, p.rows, j.s.d_head, sp.parts > 1 ? sp.out[0] + part_row(j, p, w, 0) * j.s.d_head : nullptr, [&](int r) {
+    const RowOf ro = row_of(j, r);
+    return at<T>(base, l, p.b, ro.t, p.hk * j.group + ro.g);
+  });
 }
 
 // ---- forward ------------------------------------------------------------------------------------
@@ -442,6 +466,7 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 256 ? 2 : 1) void xattn_fwd_k
   clear(o);
   float m = -INFINITY, l = 0.f;
 
+  const Mask mask = take_mask(j, p, xattn_lds + R::LDS, kbeg, kend);
   const uint32_t lds0 = lds_address(lds) + __builtin_amdgcn_readfirstlane(wave) * 1024;
   const char* const zeros = zeros_address();
   const uint32_t in_head = Source<T, DP, SW>::head_bits(dh);
@@ -453,7 +478,7 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 256 ? 2 : 1) void xattn_fwd_k
     uint64_t vis[WORDS], all = ~0ull;
 #pragma unroll
     for (int i = 0; i < WORDS; ++i) {
-      vis[i] = k0 + 64 * i < kend ? visible(j, p, k0 + 64 * i) : 0;
+      vis[i] = k0 + 64 * i < kend ? visible(j, p, mask, k0 + 64 * i) : 0;
       all &= vis[i];
     }
     const bool whole = dh == DP && (all & ALL) == ALL;
@@ -474,7 +499,7 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 256 ? 2 : 1) void xattn_fwd_k
     const T* vt = kt + ELEMS;
     wait_and_meet<(STAGES - 2) * 2 * R::N>();     // this tile is there, and nobody reads the one before it
     issue(k0 + (STAGES - 1) * TR, (buf + STAGES - 1) % STAGES);
-    const uint64_t now = visible(j, p, k0 + 32 * block);
+    const uint64_t now = visible(j, p, mask, k0 + 32 * block);
     f32x16 s[KB];
     if constexpr (KB == 2) {
       dot_rows<T, DP, true>(s[0], kt, 32 * block, q, s[1], kt, 32 * block + 32, q, lane);
@@ -562,7 +587,7 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 256 ? 2 : 1) void xattn_fwd_k
       }
     }
     __syncthreads();
-    join_waves<T, DP, SW>(j, p, w, sp, rows, stat + 256, r0, j.o, j.s.o);
+    join_queries<T, DP, SW>(j, p, w, sp, rows, [&](int row) { return stat[256 + row]; }, r0, j.o, j.s.o);
     return;
   }
   if (!mine) return;
@@ -612,6 +637,7 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) * (EXACT ? 2 : 1) <= 256 ? 2 : 1
   clear(pk);
   float rest = 0.f;                                         // sum of dz
 
+  const Mask mask = take_mask(j, p, xattn_lds + R::LDS, kbeg, kend);
   const uint32_t lds0 = lds_address(lds) + __builtin_amdgcn_readfirstlane(wave) * 1024;
   const char* const zeros = zeros_address();
   const uint32_t in_head = Source<T, DP, SW>::head_bits(dh);
@@ -623,7 +649,7 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) * (EXACT ? 2 : 1) <= 256 ? 2 : 1
     uint64_t vis[WORDS], all = ~0ull;
 #pragma unroll
     for (int i = 0; i < WORDS; ++i) {
-      vis[i] = k0 + 64 * i < kend ? visible(j, p, k0 + 64 * i) : 0;
+      vis[i] = k0 + 64 * i < kend ? visible(j, p, mask, k0 + 64 * i) : 0;
       all &= vis[i];
     }
     const bool whole = dh == DP && (all & ALL) == ALL;
@@ -664,7 +690,7 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) * (EXACT ? 2 : 1) <= 256 ? 2 : 1
     const T* vt = kt + ELEMS;
     wait_and_meet<(STAGES - 2) * 2 * R::N>();     // this tile is there, and nobody reads the one before it
     issue(k0 + (STAGES - 1) * TR, (buf + STAGES - 1) % STAGES);
-    const uint64_t now = visible(j, p, k0 + 32 * block);
+    const uint64_t now = visible(j, p, mask, k0 + 32 * block);
 #pragma unroll 1
     for (int kb = 0; kb < KB; ++kb) {
       const uint32_t seen = (uint32_t)(now >> (32 * kb)), bits = seen >> (4 * half);
@@ -687,10 +713,10 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) * (EXACT ? 2 : 1) <= 256 ? 2 : 1
   rest = pair_sum(rest);
   if constexpr (SW > 1) {
     float* rows = reinterpret_cast<float*>(xattn_lds);
-    float* stat = rows + 128 * R::JOIN_PITCH;               // [128] rests, [128] factors
+    float* stat = rows + 128 * R::JOIN_PITCH;               // [128] rests
     const int slot = wave * WR + (lane & 31);
     __syncthreads();
-    if (half == 0) { stat[slot] = rest; stat[256 + slot] = sp.parts > 1 ? 1.f : j.s.scale; }
+    if (half == 0) stat[slot] = rest;
     __syncthreads();
     rest = 0.f;
 #pragma unroll
@@ -703,7 +729,8 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) * (EXACT ? 2 : 1) <= 256 ? 2 : 1
       else j.row_delta[(int64_t)w.id * p.rows + r] = delta + rest;
       if (w.part == 0) j.row_lse[(int64_t)w.id * p.rows + r] = lse;
     }
-    join_waves<T, DP, SW>(j, p, w, sp, rows, stat + 256, r0, j.dq, j.s.dq);
+    const float f = sp.parts > 1 ? 1.f : j.s.scale;
+    join_queries<T, DP, SW>(j, p, w, sp, rows, [&](int) { return f; }, r0, j.dq, j.s.dq);
     return;
   }
   if (!mine) return;
@@ -723,18 +750,20 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) * (EXACT ? 2 : 1) <= 256 ? 2 : 1
 }
 
 // ---- backward: dk and dv ------------------------------------------------------------------------------
-template <typename T, int DP>
+template <typename T, int DP, int SW>
 __global__ __launch_bounds__(NT, DP * sizeof(T) <= 128 ? 2 : 1) void xattn_dkv_kernel(AttnJob j, AttnSplit sp) {
-  using R = Ring<T, DP, 1>;
-  constexpr int TR = R::TR, QB = TR / 32, ELEMS = R::ELEMS, STAGES = R::STAGES, BYTES = R::BYTES;
+  using R = Ring<T, DP, SW>;
+  constexpr int TR = R::TR, QB = TR / 32 / SW, RW = 4 / SW, ELEMS = R::ELEMS, STAGES = R::STAGES, BYTES = R::BYTES;
+  constexpr int WORDS = Source<T, DP, SW>::WORDS, STAT = 64 * WORDS;   // rows of statistics of a stage
   constexpr uint64_t ALL = TR >= 64 ? ~0ull : (1ull << TR) - 1;
   extern __shared__ __attribute__((aligned(16))) char xattn_lds[];
-  T* lds = reinterpret_cast<T*>(xattn_lds);                 // [STAGES][q, dO][ELEMS], then [STAGES][lse, delta][64]
+  T* lds = reinterpret_cast<T*>(xattn_lds);                 // [STAGES][q, dO][ELEMS], then [STAGES][lse, delta][STAT]
   float* stats = reinterpret_cast<float*>(lds + 2 * STAGES * ELEMS);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
   const Work w = work_of(sp);
   const Problem p = problem_of(j, w.id);
-  const int key = w.tile * (4 * WR) + wave * WR + (lane & 31);
+  const int block = __builtin_amdgcn_readfirstlane(wave) / RW * QB;       // first of this wavefront's blocks of a tile
+  const int key0 = w.tile * (RW * WR), key = key0 + wave % RW * WR + (lane & 31);
   const bool mine = key < j.s.k_rows;
   bool seen = key < p.keys;
   if (j.key_mask && seen) seen = j.key_mask[(int64_t)p.b * j.s.k_rows + key] != 0;
@@ -750,17 +779,22 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 128 ? 2 : 1) void xattn_dkv_k
   const uint32_t lds0 = lds_address(lds) + __builtin_amdgcn_readfirstlane(wave) * 1024, stats0 = lds_address(stats);
   const char* const zeros = zeros_address();
   const int beg = w.first * TR, stop = min(rows, beg + sp.per * TR);
-  const int end = w.tile * (4 * WR) < p.keys ? stop : beg;  // (a tile without a visible key: nothing but zeros to write)
-  const uint32_t in_head = Source<T, DP, 1>::head_bits(dh);
+  const int end = key0 < p.keys ? stop : beg;  // (a tile without a visible key: nothing but zeros to write)
+  const uint32_t in_head = Source<T, DP, SW>::head_bits(dh);
   const int step_t = TR / j.group, step_g = TR % j.group;
   const int64_t qstep = (step_t * j.s.q.row + step_g * j.s.q.head) * (int64_t)sizeof(T), qover = (j.s.q.row - j.group * j.s.q.head) * (int64_t)sizeof(T);
   const int64_t gstep = (step_t * j.s.d_o.row + step_g * j.s.d_o.head) * (int64_t)sizeof(T), gover = (j.s.d_o.row - j.group * j.s.d_o.head) * (int64_t)sizeof(T);
-  Source<T, DP, 1> qs, gs;
+  Source<T, DP, SW> qs, gs;
   qs.init(j, at<const T>(j.q, j.s.q, p.b, 0, p.hk * j.group), j.s.q, beg, true);
   gs.init(j, at<const T>(j.d_o, j.s.d_o, p.b, 0, p.hk * j.group), j.s.d_o, beg, true);
   auto issue = [&](int r0, int buf) {
-    const uint64_t want[1] = {first_bits(stop - r0)};
-    const bool whole = dh == DP && (want[0] & ALL) == ALL;
+    uint64_t want[WORDS], all = ~0ull;
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
+      want[i] = first_bits(stop - r0 - 64 * i);
+      all &= want[i];
+    }
+    const bool whole = dh == DP && (all & ALL) == ALL;
     qs.issue(want, in_head, whole, zeros, lds0 + buf * 2 * BYTES);
     gs.issue(want, in_head, whole, zeros, lds0 + buf * 2 * BYTES + BYTES);
     if (step_g == 0) {
@@ -770,11 +804,16 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 128 ? 2 : 1) void xattn_dkv_k
       qs.advance(qstep, qover, step_g, j.group);
       gs.advance(gstep, gover, step_g, j.group);
     }
-    // every wavefront loads the statistics of the 64 rows (the same values to the same place: all count alike)
-    const bool in = r0 + lane < stop;
-    const int64_t at_row = (int64_t)w.id * p.rows + r0 + lane;
-    lds_load4(in ? static_cast<const void*>(j.row_lse + at_row) : &g_infinity, stats0 + buf * 512);
-    lds_load4(in ? static_cast<const void*>(j.row_delta + at_row) : static_cast<const void*>(zeros), stats0 + buf * 512 + 256);
+    // every wavefront loads the statistics of the tile's rows (the same values to the same place: all count alike)
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
+      const int row = r0 + 64 * i + lane;
+      const bool in = row < stop;
+      const int64_t at_row = (int64_t)w.id * p.rows + row;
+      const uint32_t dst = stats0 + (buf * 2 * STAT + 64 * i) * 4;
+      lds_load4(in ? static_cast<const void*>(j.row_lse + at_row) : &g_infinity, dst);
+      lds_load4(in ? static_cast<const void*>(j.row_delta + at_row) : static_cast<const void*>(zeros), dst + STAT * 4);
+    }
   };
   if (beg < end) {
 #pragma unroll
@@ -788,19 +827,19 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 128 ? 2 : 1) void xattn_dkv_k
   for (int r0 = beg; r0 < end; r0 += TR, buf = (buf + 1) % STAGES) {
     const T* qt = lds + buf * 2 * ELEMS;
     const T* gt = qt + ELEMS;
-    const float* st = stats + buf * 128;
-    wait_and_meet<(STAGES - 2) * (2 * R::N + 2)>();
+    const float* st = stats + buf * 2 * STAT;
+    wait_and_meet<(STAGES - 2) * (2 * R::N + 2 * WORDS)>();
     issue(r0 + (STAGES - 1) * TR, (buf + STAGES - 1) % STAGES);
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-      if (DP <= 64 && r0 + 32 * qb >= stop) break;          // (behind the last row, the same for the whole workgroup; two blocks in one
+      if (DP * sizeof(T) <= 128 && r0 + 32 * (block + qb) >= stop) break;          // (behind the last row, the same for the whole workgroup; two blocks in one
                                                             // piece of code are worth more at 128: 650 us, with the break 720)
       f32x16 s[1], dp[1];
-      dot_rows<T, DP, true>(s[0], qt, 32 * qb, k, dp[0], gt, 32 * qb, v, lane);
+      dot_rows<T, DP, true>(s[0], qt, 32 * (block + qb), k, dp[0], gt, 32 * (block + qb), v, lane);
 #pragma unroll
       for (int gq = 0; gq < 4; ++gq) {
-        const f32x4 lse = *reinterpret_cast<const f32x4*>(st + 32 * qb + 8 * gq + 4 * half);
-        const f32x4 delta = *reinterpret_cast<const f32x4*>(st + 64 + 32 * qb + 8 * gq + 4 * half);
+        const f32x4 lse = *reinterpret_cast<const f32x4*>(st + 32 * (block + qb) + 8 * gq + 4 * half);
+        const f32x4 delta = *reinterpret_cast<const f32x4*>(st + STAT + 32 * (block + qb) + 8 * gq + 4 * half);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float pr = __builtin_amdgcn_exp2f(fminf(fmaf(s[0][4 * gq + i], c, -lse[i]), 0.f));
@@ -808,14 +847,31 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 128 ? 2 : 1) void xattn_dkv_k
           dp[0][4 * gq + i] = pr * (dp[0][4 * gq + i] - delta[i]);
         }
       }
-      dot_cols<T, DP>(dv, gt, 32 * qb, s[0], lane);
-      dot_cols<T, DP>(dk, qt, 32 * qb, dp[0], lane);
+      dot_cols<T, DP>(dv, gt, 32 * (block + qb), s[0], lane);
+      dot_cols<T, DP>(dk, qt, 32 * (block + qb), dp[0], lane);
     }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  if (!mine) return;
   // an invisible key's columns hold what its zeros gave: nothing of it is stored
   if (!seen) { clear(dk); clear(dv); }
+  if constexpr (SW > 1) {
+    float* rows = reinterpret_cast<float*>(xattn_lds);
+    const int64_t part = (((int64_t)w.part * j.s.batch * j.s.kv_heads + w.id) * j.s.k_rows) * dh;
+    const float f = sp.parts > 1 ? 1.f : j.s.scale;
+    float* slot = rows + (wave * WR + (lane & 31)) * R::JOIN_PITCH;
+    __syncthreads();                                        // nobody reads a tile any more
+    store_row<float, DP>(slot, dk, 1.f, DP, half);
+    __syncthreads();
+    join_waves<T, DP, SW>(rows, [&](int) { return f; }, key0, j.s.k_rows, dh, sp.parts > 1 ? sp.out[0] + part : nullptr,
+                          [&](int r) { return at<T>(j.dk, j.s.dk, p.b, r, p.hk); });
+    __syncthreads();
+    store_row<float, DP>(slot, dv, 1.f, DP, half);
+    __syncthreads();
+    join_waves<T, DP, SW>(rows, [&](int) { return 1.f; }, key0, j.s.k_rows, dh, sp.parts > 1 ? sp.out[1] + part : nullptr,
+                          [&](int r) { return at<T>(j.dv, j.s.dv, p.b, r, p.hk); });
+    return;
+  }
+  if (!mine) return;
   if (sp.parts > 1) {
     const int64_t row = ((int64_t)w.part * j.s.batch * j.s.kv_heads + w.id) * j.s.k_rows + key;
     store_row<float, DP>(sp.out[0] + row * dh, dk, 1.f, dh, half);
@@ -927,16 +983,17 @@ AttnSplit split_of(int64_t problems, int held, int streamed, int tile_rows, int 
   sp.parts = (all + sp.per - 1) / sp.per;
   return sp;
 }
-// The splits of the forward and dq kernels, and of the dk/dv kernel.  (fp32 heads of more than 64 elements: tiles for four wavefronts
-// would not fit the LDS.)
+// fp32 heads of more than 64 elements: tiles for four wavefronts would not fit the LDS.
+int most_sw(const vf_attn_shape& s) { return s.dtype == VF_BF16 || s.d_head <= 64 ? 4 : 2; }
+// The splits of the forward and dq kernels, and of the dk/dv kernel.
 AttnSplit split_rows(const vf_attn_shape& s) {
   const bool b = s.dtype == VF_BF16;
   return split_of((int64_t)s.batch * s.kv_heads, s.q_heads / s.kv_heads * s.q_rows, s.k_rows, b ? Elem<bf16_t>::TR : Elem<float>::TR,
-                  b || s.d_head <= 64 ? 4 : 2, b);
+                  most_sw(s), b);
 }
 AttnSplit split_keys(const vf_attn_shape& s) {
   const bool b = s.dtype == VF_BF16;
-  return split_of((int64_t)s.batch * s.kv_heads, s.k_rows, s.q_heads / s.kv_heads * s.q_rows, b ? Elem<bf16_t>::TR : Elem<float>::TR, 1, b);
+  return split_of((int64_t)s.batch * s.kv_heads, s.k_rows, s.q_heads / s.kv_heads * s.q_rows, b ? Elem<bf16_t>::TR : Elem<float>::TR, most_sw(s), b);
 }
 int64_t round4(int64_t floats) { return (floats + 3) & ~int64_t(3); }
 // Floats of the parts of a pass over the rows (results and two statistics a row), and over the keys (dk and dv).
@@ -967,7 +1024,7 @@ int launch_join(const AttnJob& j, const AttnSplit& sp, int64_t rows, hipStream_t
 
 template <typename T, int DP, int SW>
 int launch_fwd(const AttnJob& j, const AttnSplit& sp, hipStream_t st) {
-  constexpr int lds = std::max(Ring<T, DP, SW>::LDS, Ring<T, DP, SW>::JOIN);
+  constexpr int lds = std::max(Ring<T, DP, SW>::LDS + kMaskWords * 8, Ring<T, DP, SW>::JOIN);
   static std::atomic<uint64_t> ready{0};
   VF_TRY(allow_lds(reinterpret_cast<const void*>(&xattn_fwd_kernel<T, DP, SW>), lds, ready));
   xattn_fwd_kernel<T, DP, SW><<<dim3(j.s.batch * j.s.kv_heads, sp.tiles, sp.parts), NT, lds, st>>>(j, sp);
@@ -977,7 +1034,7 @@ int launch_fwd(const AttnJob& j, const AttnSplit& sp, hipStream_t st) {
 constexpr int kExactKeys = 512;
 template <typename T, int DP, int SW, bool EXACT>
 int launch_dq_of(const AttnJob& j, const AttnSplit& sp, hipStream_t st) {
-  constexpr int lds = std::max(Ring<T, DP, SW>::LDS, Ring<T, DP, SW>::JOIN);
+  constexpr int lds = std::max(Ring<T, DP, SW>::LDS + kMaskWords * 8, Ring<T, DP, SW>::JOIN);
   static std::atomic<uint64_t> ready{0};
   VF_TRY(allow_lds(reinterpret_cast<const void*>(&xattn_dq_kernel<T, DP, SW, EXACT>), lds, ready));
   xattn_dq_kernel<T, DP, SW, EXACT><<<dim3(j.s.batch * j.s.kv_heads, sp.tiles, sp.parts), NT, lds, st>>>(j, sp);
@@ -990,12 +1047,13 @@ int launch_dq(const AttnJob& j, const AttnSplit& sp, hipStream_t st) {
   if constexpr (sizeof(T) == 2) return j.s.k_rows <= kExactKeys ? launch_dq_of<T, DP, SW, true>(j, sp, st) : launch_dq_of<T, DP, SW, false>(j, sp, st);
   else return launch_dq_of<T, DP, SW, false>(j, sp, st);
 }
-template <typename T, int DP>
+template <typename T, int DP, int SW>
 int launch_dkv(const AttnJob& j, const AttnSplit& sp, hipStream_t st) {
-  constexpr int lds = Ring<T, DP, 1>::LDS + Ring<T, DP, 1>::STAGES * 512;
+  using R = Ring<T, DP, SW>;
+  constexpr int lds = std::max(R::LDS + R::STAGES * 8 * std::max(64, R::TR), R::JOIN);
   static std::atomic<uint64_t> ready{0};
-  VF_TRY(allow_lds(reinterpret_cast<const void*>(&xattn_dkv_kernel<T, DP>), lds, ready));
-  xattn_dkv_kernel<T, DP><<<dim3(j.s.batch * j.s.kv_heads, sp.tiles, sp.parts), NT, lds, st>>>(j, sp);
+  VF_TRY(allow_lds(reinterpret_cast<const void*>(&xattn_dkv_kernel<T, DP, SW>), lds, ready));
+  xattn_dkv_kernel<T, DP, SW><<<dim3(j.s.batch * j.s.kv_heads, sp.tiles, sp.parts), NT, lds, st>>>(j, sp);
   VF_LAUNCH_CHECK();
   return VF_OK;
 }
@@ -1021,7 +1079,11 @@ int pass_keys(const AttnJob& j, float* ws, hipStream_t st) {
   AttnSplit sp = split_keys(j.s);
   sp.out[0] = ws;
   sp.out[1] = ws + sp.parts * rows * j.s.d_head;
-  VF_TRY((launch_dkv<T, DP>(j, sp, st)));
+  if constexpr (sizeof(T) == 2 || DP <= 64) {
+    if (sp.sw == 4) VF_TRY((launch_dkv<T, DP, 4>(j, sp, st)));
+  }
+  if (sp.sw == 2) VF_TRY((launch_dkv<T, DP, 2>(j, sp, st)));
+  if (sp.sw == 1) VF_TRY((launch_dkv<T, DP, 1>(j, sp, st)));
   return sp.parts > 1 ? launch_join<T, 2>(j, sp, rows, st) : VF_OK;
 }
 template <typename T, int DP>
@@ -1047,7 +1109,9 @@ int64_t attn_workspace_bytes(const vf_attn_shape& s, bool backward) {
 static int make_bits(AttnJob& j, float* ws, hipStream_t st) {
   j.words = (int)mask_words(j.s);
   const int64_t n = (int64_t)j.s.batch * j.words;
-  if (!j.key_mask || !n) return VF_OK;
+  const AttnSplit sp = split_rows(j.s);
+  const int tile = std::max(j.s.dtype == VF_BF16 ? Elem<bf16_t>::TR : Elem<float>::TR, 32 * sp.sw);
+  if (!j.key_mask || !n || !j.s.q_rows || (int64_t)sp.per * tile <= kMaskWords * 64) return VF_OK;
   j.bits = reinterpret_cast<uint64_t*>(ws);
   mask_bits_kernel<<<(unsigned)((n + NT / 64 - 1) / (NT / 64)), NT, 0, st>>>(j.key_mask, j.s.k_rows, j.words, n, reinterpret_cast<uint64_t*>(ws));
   VF_LAUNCH_CHECK();

@@ -416,7 +416,8 @@ def test_attention_over_padded_batches(B, Tq, Tk, Hq, Hk, dh, q_len, k_len, dtyp
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("B,Tq,Tk,Hq,Hk,dh", [(4, 50, 211, 2, 2, 64), (3, 1, 333, 4, 2, 128), (4, 140, 64, 2, 1, 40), (3, 3, 1500, 2, 2, 64)])
+@pytest.mark.parametrize("B,Tq,Tk,Hq,Hk,dh", [(4, 50, 211, 2, 2, 64), (3, 1, 333, 4, 2, 128), (4, 140, 64, 2, 1, 40), (3, 3, 1500, 2, 2, 64),
+                                              (64, 1, 4200, 4, 4, 64)])
 def test_attention_with_key_masks(B, Tq, Tk, Hq, Hk, dh, dtype):
     """Single keys masked out, one sample that sees nothing, one that sees its last key alone, with lengths on top."""
     import torch
