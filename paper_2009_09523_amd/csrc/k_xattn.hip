@@ -14,6 +14,7 @@
 // are read once for all of them and the gradients of shared keys are summed in registers.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "vf_device.h"
 
@@ -29,6 +30,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int NT = 256;                                     // four wavefronts
 constexpr int WR = 32;                                      // held rows of a wavefront
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kSlack = 8.f;                              // see the forward kernel
 constexpr float kFar = 1048576.f;                          // log2 units from which 2^-24 of a score is no longer far below 1
 
 // row of register r in a 32 x 32 accumulator tile
@@ -100,7 +102,7 @@ __device__ __forceinline__ void step_of(f32x16& acc, u32x4 x, u32x4 y) {
     for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(u[e], v[e], acc, 0, 0, 0);
   }
 }
-template <typename T, int DP, bool TWO, int AHEAD = 4>
+template <typename T, int DP, bool TWO, int AHEAD = 4, int BESIDE = 0>
 __device__ __forceinline__ void dot_rows(f32x16& accA, const T* ta, int ra, const Held<T, DP>& a, f32x16& accB, const T* tb, int rb,
                                          const Held<T, DP>& b, int lane) {
   constexpr int S = Held<T, DP>::STEPS, LOOK = S < AHEAD ? S : AHEAD, PAIR = TWO ? 2 : 1, OPS = PAIR * (sizeof(T) == 2 ? 1 : 4);
@@ -125,8 +127,17 @@ __device__ __forceinline__ void dot_rows(f32x16& accA, const T* ta, int ra, cons
   for (int s = 0; s < S - LOOK; ++s) {
     __builtin_amdgcn_sched_group_barrier(0x8, OPS, 0);             // matrix instructions
     __builtin_amdgcn_sched_group_barrier(0x100, PAIR, 0);
+    if constexpr (BESIDE > 0) __builtin_amdgcn_sched_group_barrier(0x2, BESIDE * PAIR, 0);   // vector instructions
   }
-  __builtin_amdgcn_sched_group_barrier(0x8, OPS * LOOK, 0);
+  if constexpr (BESIDE > 0) {
+#pragma unroll
+    for (int s = 0; s < LOOK; ++s) {
+      __builtin_amdgcn_sched_group_barrier(0x8, OPS, 0);
+      __builtin_amdgcn_sched_group_barrier(0x2, BESIDE * PAIR, 0);
+    }
+  } else {
+    __builtin_amdgcn_sched_group_barrier(0x8, OPS * LOOK, 0);
+  }
 }
 
 // Transposing read: elements (row0 + 4 half + 0..3, col0 + l % 32) and the same eight rows further down.
@@ -204,6 +215,9 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_
 __device__ __forceinline__ void lds_load16(const void* src, uint32_t dst) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(src) : "memory");
 }
+__device__ __forceinline__ void lds_load16(const char* base, uint32_t off, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(off), "s"(base) : "memory");
+}
 __device__ __forceinline__ void lds_load4(const void* src, uint32_t dst) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(dst), "v"(src) : "memory");
 }
@@ -244,8 +258,9 @@ __device__ __forceinline__ Problem problem_of(const AttnJob& j, int id) {
   p.b = id / j.s.kv_heads;
   p.hk = id - p.b * j.s.kv_heads;
   p.rows = j.group * j.s.q_rows;
-  p.q_len = j.q_len ? __builtin_amdgcn_readfirstlane(min(max(j.q_len[p.b], 0), j.s.q_rows)) : j.s.q_rows;
-  p.keys = j.k_len ? __builtin_amdgcn_readfirstlane(min(max(j.k_len[p.b], 0), j.s.k_rows)) : j.s.k_rows;
+  typedef const __attribute__((address_space(4))) int32_t* scalar;        // (the same for all: scalar loads)
+  p.q_len = j.q_len ? min(max(((scalar)j.q_len)[p.b], 0), j.s.q_rows) : j.s.q_rows;
+  p.keys = j.k_len ? min(max(((scalar)j.k_len)[p.b], 0), j.s.k_rows) : j.s.k_rows;
   return p;
 }
 // query and head (among the group's) of row r
@@ -260,58 +275,59 @@ __device__ __forceinline__ T* at(const void* base, const vf_attn_layout& l, int 
   return const_cast<T*>(static_cast<const T*>(base)) + (int64_t)b * l.batch + (int64_t)row * l.row + (int64_t)head * l.head;
 }
 
-// This thread's chunks of one streamed tensor: where they lie for the tile that is loaded next.
-template <typename T, int DP, int SW>
+// This thread's chunks of one streamed tensor.  Row r of the problem is head r % group of row r / group (GROUPED), or row r.
+// Where the rows of a tile lie within 32 bits of its first one, and every tile starts with the group's first head, a tile's
+// addresses are a scalar that moves on and offsets that stay (`near`): no vector instruction for a whole tile.
+template <typename T, int DP, int SW, bool GROUPED>
 struct Source {
-  static constexpr int N = Ring<T, DP, SW>::N, CH = Ring<T, DP, SW>::CH, WORDS = (Ring<T, DP, SW>::TR + 63) / 64;
+  static constexpr int N = Ring<T, DP, SW>::N, CH = Ring<T, DP, SW>::CH, TR = Ring<T, DP, SW>::TR, WORDS = (TR + 63) / 64;
   static_assert(64 % (NT / CH) == 0, "rows of a load within one word of bits");
-  const char* p[N];
-  int g[N];                     // head among the group's (rows of several heads; else 0)
-  // base: head 0 of row 0; rows r0, r0 + 1, ... are head r % group of row r / group
-  __device__ __forceinline__ void init(const AttnJob& j, const T* base, const vf_attn_layout& l, int r0, bool grouped) {
+  const char* base;             // head 0 of row 0
+  int64_t row_b, head_b;        // strides in bytes
+  bool near;
+  uint32_t off[N];
+  static __device__ __forceinline__ int row(int i) { return (i * NT + (int)threadIdx.x) / CH; }
+  // first element of chunk i in its row (the exchange of places undoes itself)
+  static __device__ __forceinline__ int elem(int i) { return Tile<T, DP>::pos(row(i), (i * NT + (int)threadIdx.x) % CH) - row(i) * DP; }
+  __device__ __forceinline__ void init(const AttnJob& j, const T* first, const vf_attn_layout& l) {
+    base = reinterpret_cast<const char*>(first);
+    row_b = l.row * (int64_t)sizeof(T);
+    head_b = l.head * (int64_t)sizeof(T);
+    near = row_b >= 0 && (!GROUPED || head_b >= 0) && TR * row_b + (GROUPED ? j.group * head_b : 0) < (1ll << 31) && (!GROUPED || TR % j.group == 0);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int r = (i * NT + (int)threadIdx.x) / CH;
-      const RowOf ro = grouped ? row_of(j, r0 + r) : RowOf{r0 + r, 0};
-      const int c = Tile<T, DP>::pos(r, (i * NT + (int)threadIdx.x) % CH) - r * DP;   // (the exchange of places undoes itself)
-      p[i] = reinterpret_cast<const char*>(base + (int64_t)ro.t * l.row + (int64_t)ro.g * l.head + c);
-      g[i] = ro.g;
+      const RowOf ro = GROUPED ? row_of(j, row(i)) : RowOf{row(i), 0};
+      off[i] = (near ? (uint32_t)ro.t * (uint32_t)row_b + (uint32_t)ro.g * (uint32_t)head_b : 0) + elem(i) * (uint32_t)sizeof(T);
     }
   }
   // bit i: chunk i lies within the head
   static __device__ __forceinline__ uint32_t head_bits(int dh) {
     uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int r = (i * NT + (int)threadIdx.x) / CH;
-      if (Tile<T, DP>::pos(r, (i * NT + (int)threadIdx.x) % CH) - r * DP < dh) m |= 1u << i;
-    }
+    for (int i = 0; i < N; ++i)
+      if (elem(i) < dh) m |= 1u << i;
     return m;
   }
-  // rows: bit r: row r of the tile is wanted; tile: LDS address of the tile's buffer for this wavefront
-  __device__ __forceinline__ void issue(const uint64_t (&rows)[WORDS], uint32_t head, bool whole, const char* zeros, uint32_t tile) const {
+  // Tile from row r0 on.  rows: bit r: row r of the tile is wanted; whole: all of them, and the head fills its chunks; tile: LDS
+  // address of the tile's buffer for this wavefront
+  __device__ __forceinline__ void issue(const AttnJob& j, int r0, const uint64_t (&rows)[WORDS], uint32_t head, bool whole, const char* zeros,
+                                        uint32_t tile) const {
+    const RowOf first = GROUPED ? row_of(j, r0) : RowOf{r0, 0};
+    const char* from = base + first.t * row_b;
+    if (near && whole) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const char* src = p[i];
-      if (!whole) {
-        const uint64_t mine = rows[i * (NT / CH) / 64] >> (threadIdx.x / CH);
-        src = ((mine >> (i * (NT / CH) % 64)) & (head >> i) & 1) ? p[i] : zeros;
-      }
-      lds_load16(src, tile + i * (NT * 16));
+      for (int i = 0; i < N; ++i) lds_load16(from, off[i], tile + i * (NT * 16));
+      return;
     }
-  }
-  __device__ __forceinline__ void advance(int64_t step) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) p[i] += step;
-  }
-  // rows of several heads: step for TR / group rows and TR % group heads, and one more row where the heads run over
-  __device__ __forceinline__ void advance(int64_t step, int64_t over, int heads, int group) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      g[i] += heads;
-      const bool wrap = g[i] >= group;
-      p[i] += step + (wrap ? over : 0);
-      if (wrap) g[i] -= group;
+      const char* p = from + off[i];
+      if (!near) {
+        const RowOf ro = GROUPED ? row_of(j, r0 + row(i)) : RowOf{r0 + row(i), 0};
+        p = base + ro.t * row_b + ro.g * head_b + off[i];
+      }
+      const uint64_t mine = rows[i * (NT / CH) / 64] >> (threadIdx.x / CH);
+      lds_load16(((mine >> (i * (NT / CH) % 64)) & (head >> i) & 1) ? p : zeros, tile + i * (NT * 16));
     }
   }
 };
@@ -364,6 +380,12 @@ __global__ __launch_bounds__(NT) void mask_bits_kernel(const uint8_t* __restrict
   const int k = (int)(w - b * words) * 64 + (threadIdx.x & 63);
   const uint64_t on = __ballot(k < keys && mask[b * keys + k] != 0);
   if ((threadIdx.x & 63) == 0) bits[w] = on;
+}
+
+// p of a score: at most 1 also where scores lie so far out that the rounding of lse passes 1.  (The bound is the instruction's own:
+// clamped to [0, 1].)
+__device__ __forceinline__ float weight_of(float s, float c, float lse) {
+  return __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(fmaf(s, c, -lse)), 0.f, 1.f);
 }
 
 // max / sum over the two lanes of a column
@@ -444,7 +466,7 @@ template <typename T, int DP, int SW>
 __global__ __launch_bounds__(NT, DP * sizeof(T) <= 256 ? 2 : 1) void xattn_fwd_kernel(AttnJob j, AttnSplit sp) {
   using R = Ring<T, DP, SW>;
   constexpr int TR = R::TR, KB = TR / 32 / SW, RW = 4 / SW, ELEMS = R::ELEMS, STAGES = R::STAGES, BYTES = R::BYTES;
-  constexpr int WORDS = Source<T, DP, SW>::WORDS;
+  constexpr int WORDS = Source<T, DP, SW, false>::WORDS;
   constexpr uint64_t ALL = TR >= 64 ? ~0ull : (1ull << TR) - 1, MINE = KB == 2 ? ~0ull : 0xffffffffull;
   extern __shared__ __attribute__((aligned(16))) char xattn_lds[];
   T* lds = reinterpret_cast<T*>(xattn_lds);                 // [STAGES][k, v][ELEMS]
@@ -464,16 +486,16 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 256 ? 2 : 1) void xattn_fwd_k
   Held<T, DP> q;
   f32x16 o[DP / 32];
   clear(o);
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY, l = 0.f, ref = 0.f, base = 0.f;
+  bool far = false;
 
   const Mask mask = take_mask(j, p, xattn_lds + R::LDS, kbeg, kend);
   const uint32_t lds0 = lds_address(lds) + __builtin_amdgcn_readfirstlane(wave) * 1024;
   const char* const zeros = zeros_address();
-  const uint32_t in_head = Source<T, DP, SW>::head_bits(dh);
-  const int64_t kstep = TR * j.s.k.row * (int64_t)sizeof(T), vstep = TR * j.s.v.row * (int64_t)sizeof(T);
-  Source<T, DP, SW> ks, vs;
-  ks.init(j, at<const T>(j.k, j.s.k, p.b, 0, p.hk), j.s.k, kbeg, false);
-  vs.init(j, at<const T>(j.v, j.s.v, p.b, 0, p.hk), j.s.v, kbeg, false);
+  const uint32_t in_head = Source<T, DP, SW, false>::head_bits(dh);
+  Source<T, DP, SW, false> ks, vs;
+  ks.init(j, at<const T>(j.k, j.s.k, p.b, 0, p.hk), j.s.k);
+  vs.init(j, at<const T>(j.v, j.s.v, p.b, 0, p.hk), j.s.v);
   auto issue = [&](int k0, int buf) {                       // (behind the last tile: zeros, so that every tile counts alike)
     uint64_t vis[WORDS], all = ~0ull;
 #pragma unroll
@@ -482,10 +504,8 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 256 ? 2 : 1) void xattn_fwd_k
       all &= vis[i];
     }
     const bool whole = dh == DP && (all & ALL) == ALL;
-    ks.issue(vis, in_head, whole, zeros, lds0 + buf * 2 * BYTES);
-    vs.issue(vis, in_head, whole, zeros, lds0 + buf * 2 * BYTES + BYTES);
-    ks.advance(kstep);
-    vs.advance(vstep);
+    ks.issue(j, k0, vis, in_head, whole, zeros, lds0 + buf * 2 * BYTES);
+    vs.issue(j, k0, vis, in_head, whole, zeros, lds0 + buf * 2 * BYTES + BYTES);
   };
   if (kbeg < kend) {
 #pragma unroll
@@ -493,8 +513,7 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 256 ? 2 : 1) void xattn_fwd_k
   }
   q.load(live ? at<const T>(j.q, j.s.q, p.b, ro.t, head) : nullptr, dh, half);
   q.arrive();
-  int buf = 0;
-  for (int k0 = kbeg; k0 < kend; k0 += TR, buf = (buf + 1) % STAGES) {
+  auto step = [&](auto buf, int k0) {
     const T* kt = lds + buf * 2 * ELEMS;
     const T* vt = kt + ELEMS;
     wait_and_meet<(STAGES - 2) * 2 * R::N>();     // this tile is there, and nobody reads the one before it
@@ -521,14 +540,25 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 256 ? 2 : 1) void xattn_fwd_k
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
-    const float mn = fmaxf(m, pair_max(top));
-    const float ref = mn == -INFINITY ? 0.f : mn;           // no visible key so far: every p is exp2(-inf) = 0
-    const float fade = __builtin_amdgcn_exp2f((m - ref) * c);
-    const float base = ref * c;
-    m = mn;
+    // The reference m of a row's exponentials follows its maximum only when some row's has passed it by kSlack: until then no p
+    // exceeds 2^kSlack and nothing is rescaled.  (2 x 16 problems of 4096 x 8192 x 128: 556 -> 540 us against always.)
+    const float mt = pair_max(top);
+    if (__any((mt - m) * c > kSlack)) {
+      const float mn = fmaxf(m, mt);
+      const float fade = __builtin_amdgcn_exp2f((m - (mn == -INFINITY ? 0.f : mn)) * c);
+      m = mn;
+      ref = mn == -INFINITY ? 0.f : mn;                     // no visible key so far: every p is exp2(-inf) = 0
+      base = ref * c;
+      far = __any(fabsf(base) > kFar);
+      l *= fade;
+#pragma unroll
+      for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[db][i] *= fade;
+    }
     // s c - base in one operation keeps the rounding of base: nothing as long as that is far below 1, and the same
     // factor for all of a row; where it is not, the difference is taken first.
-    if (__any(fabsf(base) > kFar)) {
+    if (far) {
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -544,15 +574,19 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 256 ? 2 : 1) void xattn_fwd_k
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) sum += s[kb][i];
-    l = l * fade + sum;
-    if (__any(fade != 1.f)) {                               // (most tiles bring no row a new maximum)
-#pragma unroll
-      for (int db = 0; db < DP / 32; ++db)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[db][i] *= fade;
-    }
+    l += sum;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) dot_cols<T, DP>(o, vt, 32 * (block + kb), s[kb], lane);
+  };
+  if constexpr (SW == 1 && STAGES == 2) {                   // (buffers known where the code is made: no address is computed in the loop)
+    for (int k0 = kbeg; k0 < kend; k0 += TR) {
+      step(std::integral_constant<int, 0>(), k0);
+      if ((k0 += TR) >= kend) break;
+      step(std::integral_constant<int, 1>(), k0);
+    }
+  } else {
+    int buf = 0;
+    for (int k0 = kbeg; k0 < kend; k0 += TR, buf = (buf + 1) % STAGES) step(buf, k0);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // no load may find its LDS given away
   l = pair_sum(l);
@@ -613,7 +647,7 @@ template <typename T, int DP, int SW, bool EXACT>
 __global__ __launch_bounds__(NT, DP * sizeof(T) * (EXACT ? 2 : 1) <= 256 ? 2 : 1) void xattn_dq_kernel(AttnJob j, AttnSplit sp) {
   using R = Ring<T, DP, SW>;
   constexpr int TR = R::TR, KB = TR / 32 / SW, RW = 4 / SW, ELEMS = R::ELEMS, STAGES = R::STAGES, BYTES = R::BYTES;
-  constexpr int WORDS = Source<T, DP, SW>::WORDS;
+  constexpr int WORDS = Source<T, DP, SW, false>::WORDS;
   constexpr uint64_t ALL = TR >= 64 ? ~0ull : (1ull << TR) - 1, MINE = KB == 2 ? ~0ull : 0xffffffffull;
   extern __shared__ __attribute__((aligned(16))) char xattn_lds[];
   T* lds = reinterpret_cast<T*>(xattn_lds);
@@ -640,11 +674,10 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) * (EXACT ? 2 : 1) <= 256 ? 2 : 1
   const Mask mask = take_mask(j, p, xattn_lds + R::LDS, kbeg, kend);
   const uint32_t lds0 = lds_address(lds) + __builtin_amdgcn_readfirstlane(wave) * 1024;
   const char* const zeros = zeros_address();
-  const uint32_t in_head = Source<T, DP, SW>::head_bits(dh);
-  const int64_t kstep = TR * j.s.k.row * (int64_t)sizeof(T), vstep = TR * j.s.v.row * (int64_t)sizeof(T);
-  Source<T, DP, SW> ks, vs;
-  ks.init(j, at<const T>(j.k, j.s.k, p.b, 0, p.hk), j.s.k, kbeg, false);
-  vs.init(j, at<const T>(j.v, j.s.v, p.b, 0, p.hk), j.s.v, kbeg, false);
+  const uint32_t in_head = Source<T, DP, SW, false>::head_bits(dh);
+  Source<T, DP, SW, false> ks, vs;
+  ks.init(j, at<const T>(j.k, j.s.k, p.b, 0, p.hk), j.s.k);
+  vs.init(j, at<const T>(j.v, j.s.v, p.b, 0, p.hk), j.s.v);
   auto issue = [&](int k0, int buf) {                       // (behind the last tile: zeros, so that every tile counts alike)
     uint64_t vis[WORDS], all = ~0ull;
 #pragma unroll
@@ -653,10 +686,8 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) * (EXACT ? 2 : 1) <= 256 ? 2 : 1
       all &= vis[i];
     }
     const bool whole = dh == DP && (all & ALL) == ALL;
-    ks.issue(vis, in_head, whole, zeros, lds0 + buf * 2 * BYTES);
-    vs.issue(vis, in_head, whole, zeros, lds0 + buf * 2 * BYTES + BYTES);
-    ks.advance(kstep);
-    vs.advance(vstep);
+    ks.issue(j, k0, vis, in_head, whole, zeros, lds0 + buf * 2 * BYTES);
+    vs.issue(j, k0, vis, in_head, whole, zeros, lds0 + buf * 2 * BYTES + BYTES);
   };
   if (kbeg < kend) {
 #pragma unroll
@@ -684,8 +715,7 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) * (EXACT ? 2 : 1) <= 256 ? 2 : 1
   }
   q.arrive();
   g.arrive();
-  int buf = 0;
-  for (int k0 = kbeg; k0 < kend; k0 += TR, buf = (buf + 1) % STAGES) {
+  auto step = [&](auto buf, int k0) {
     const T* kt = lds + buf * 2 * ELEMS;
     const T* vt = kt + ELEMS;
     wait_and_meet<(STAGES - 2) * 2 * R::N>();     // this tile is there, and nobody reads the one before it
@@ -693,21 +723,38 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) * (EXACT ? 2 : 1) <= 256 ? 2 : 1
     const uint64_t now = visible(j, p, mask, k0 + 32 * block);
 #pragma unroll 1
     for (int kb = 0; kb < KB; ++kb) {
-      const uint32_t seen = (uint32_t)(now >> (32 * kb)), bits = seen >> (4 * half);
+      const uint32_t seen = (uint32_t)(now >> (32 * kb));
       if (seen == 0) continue;                              // (the same for the whole wavefront)
       f32x16 s, dp, pr;
       dot_rows<T, DP, true, 2>(s, kt, 32 * (block + kb), q, dp, vt, 32 * (block + kb), g, lane);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        float x = __builtin_amdgcn_exp2f(fminf(fmaf(s[i], c, -lse), 0.f));   // (scores so far out that the rounding of lse passes 1)
-        if (!((bits >> acc_row(i, 0)) & 1)) x = 0.f;
-        pr[i] = x;
-        s[i] = x * (dp[i] - delta);
+        pr[i] = weight_of(s[i], c, lse);
+      }
+      if (seen != 0xffffffffu) {
+        const uint32_t bits = seen >> (4 * half);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (!((bits >> acc_row(i, 0)) & 1)) pr[i] = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[i] = pr[i] * (dp[i] - delta);
         rest += s[i];
       }
       if constexpr (EXACT) dot_cols<T, DP, true>(dq, kt, 32 * (block + kb), s, lane, &pk, &pr);
       else dot_cols<T, DP>(dq, kt, 32 * (block + kb), s, lane);
     }
+  };
+  if constexpr (SW == 1 && STAGES == 2) {                   // (buffers known where the code is made: no address is computed in the loop)
+    for (int k0 = kbeg; k0 < kend; k0 += TR) {
+      step(std::integral_constant<int, 0>(), k0);
+      if ((k0 += TR) >= kend) break;
+      step(std::integral_constant<int, 1>(), k0);
+    }
+  } else {
+    int buf = 0;
+    for (int k0 = kbeg; k0 < kend; k0 += TR, buf = (buf + 1) % STAGES) step(buf, k0);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   rest = pair_sum(rest);
@@ -754,7 +801,9 @@ template <typename T, int DP, int SW>
 __global__ __launch_bounds__(NT, DP * sizeof(T) <= 128 ? 2 : 1) void xattn_dkv_kernel(AttnJob j, AttnSplit sp) {
   using R = Ring<T, DP, SW>;
   constexpr int TR = R::TR, QB = TR / 32 / SW, RW = 4 / SW, ELEMS = R::ELEMS, STAGES = R::STAGES, BYTES = R::BYTES;
-  constexpr int WORDS = Source<T, DP, SW>::WORDS, STAT = 64 * WORDS;   // rows of statistics of a stage
+  constexpr int WORDS = Source<T, DP, SW, false>::WORDS, STAT = 64 * WORDS;   // rows of statistics of a stage
+  constexpr bool BOTH = false;
+  constexpr int UNROLL = DP * sizeof(T) <= 128 ? 1 : 2, BESIDE = 6;
   constexpr uint64_t ALL = TR >= 64 ? ~0ull : (1ull << TR) - 1;
   extern __shared__ __attribute__((aligned(16))) char xattn_lds[];
   T* lds = reinterpret_cast<T*>(xattn_lds);                 // [STAGES][q, dO][ELEMS], then [STAGES][lse, delta][STAT]
@@ -780,13 +829,10 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 128 ? 2 : 1) void xattn_dkv_k
   const char* const zeros = zeros_address();
   const int beg = w.first * TR, stop = min(rows, beg + sp.per * TR);
   const int end = key0 < p.keys ? stop : beg;  // (a tile without a visible key: nothing but zeros to write)
-  const uint32_t in_head = Source<T, DP, SW>::head_bits(dh);
-  const int step_t = TR / j.group, step_g = TR % j.group;
-  const int64_t qstep = (step_t * j.s.q.row + step_g * j.s.q.head) * (int64_t)sizeof(T), qover = (j.s.q.row - j.group * j.s.q.head) * (int64_t)sizeof(T);
-  const int64_t gstep = (step_t * j.s.d_o.row + step_g * j.s.d_o.head) * (int64_t)sizeof(T), gover = (j.s.d_o.row - j.group * j.s.d_o.head) * (int64_t)sizeof(T);
-  Source<T, DP, SW> qs, gs;
-  qs.init(j, at<const T>(j.q, j.s.q, p.b, 0, p.hk * j.group), j.s.q, beg, true);
-  gs.init(j, at<const T>(j.d_o, j.s.d_o, p.b, 0, p.hk * j.group), j.s.d_o, beg, true);
+  const uint32_t in_head = Source<T, DP, SW, false>::head_bits(dh);
+  Source<T, DP, SW, true> qs, gs;
+  qs.init(j, at<const T>(j.q, j.s.q, p.b, 0, p.hk * j.group), j.s.q);
+  gs.init(j, at<const T>(j.d_o, j.s.d_o, p.b, 0, p.hk * j.group), j.s.d_o);
   auto issue = [&](int r0, int buf) {
     uint64_t want[WORDS], all = ~0ull;
 #pragma unroll
@@ -795,15 +841,8 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 128 ? 2 : 1) void xattn_dkv_k
       all &= want[i];
     }
     const bool whole = dh == DP && (all & ALL) == ALL;
-    qs.issue(want, in_head, whole, zeros, lds0 + buf * 2 * BYTES);
-    gs.issue(want, in_head, whole, zeros, lds0 + buf * 2 * BYTES + BYTES);
-    if (step_g == 0) {
-      qs.advance(qstep);
-      gs.advance(gstep);
-    } else {
-      qs.advance(qstep, qover, step_g, j.group);
-      gs.advance(gstep, gover, step_g, j.group);
-    }
+    qs.issue(j, r0, want, in_head, whole, zeros, lds0 + buf * 2 * BYTES);
+    gs.issue(j, r0, want, in_head, whole, zeros, lds0 + buf * 2 * BYTES + BYTES);
     // every wavefront loads the statistics of the tile's rows (the same values to the same place: all count alike)
 #pragma unroll
     for (int i = 0; i < WORDS; ++i) {
@@ -823,34 +862,60 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 128 ? 2 : 1) void xattn_dkv_k
   v.load(seen ? at<const T>(j.v, j.s.v, p.b, key, p.hk) : nullptr, dh, half);
   k.arrive();
   v.arrive();
-  int buf = 0;
-  for (int r0 = beg; r0 < end; r0 += TR, buf = (buf + 1) % STAGES) {
+  auto step = [&](auto buf, int r0) {
     const T* qt = lds + buf * 2 * ELEMS;
     const T* gt = qt + ELEMS;
     const float* st = stats + buf * 2 * STAT;
     wait_and_meet<(STAGES - 2) * (2 * R::N + 2 * WORDS)>();
     issue(r0 + (STAGES - 1) * TR, (buf + STAGES - 1) % STAGES);
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-      if (DP * sizeof(T) <= 128 && r0 + 32 * (block + qb) >= stop) break;          // (behind the last row, the same for the whole workgroup; two blocks in one
-                                                            // piece of code are worth more at 128: 650 us, with the break 720)
-      f32x16 s[1], dp[1];
-      dot_rows<T, DP, true>(s[0], qt, 32 * (block + qb), k, dp[0], gt, 32 * (block + qb), v, lane);
+    // p, dz of 32 rows from their products
+    auto weights = [&](f32x16& s, f32x16& dp, int row0) {
 #pragma unroll
       for (int gq = 0; gq < 4; ++gq) {
-        const f32x4 lse = *reinterpret_cast<const f32x4*>(st + 32 * (block + qb) + 8 * gq + 4 * half);
-        const f32x4 delta = *reinterpret_cast<const f32x4*>(st + STAT + 32 * (block + qb) + 8 * gq + 4 * half);
+        const f32x4 lse = *reinterpret_cast<const f32x4*>(st + row0 + 8 * gq + 4 * half);
+        const f32x4 delta = *reinterpret_cast<const f32x4*>(st + STAT + row0 + 8 * gq + 4 * half);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float pr = __builtin_amdgcn_exp2f(fminf(fmaf(s[0][4 * gq + i], c, -lse[i]), 0.f));
-          s[0][4 * gq + i] = pr;
-          dp[0][4 * gq + i] = pr * (dp[0][4 * gq + i] - delta[i]);
+          const float pr = weight_of(s[4 * gq + i], c, lse[i]);
+          s[4 * gq + i] = pr;
+          dp[4 * gq + i] = pr * (dp[4 * gq + i] - delta[i]);
         }
       }
-      dot_cols<T, DP>(dv, gt, 32 * (block + qb), s[0], lane);
-      dot_cols<T, DP>(dk, qt, 32 * (block + qb), dp[0], lane);
+    };
+    if constexpr (BOTH) {
+      // Two blocks of 32 rows, one wavefront to a SIMD: the vector work of the first goes between the matrix instructions of the
+      // second, and that of the second between those that take the first one's results.
+      f32x16 s0, p0, s1, p1;
+      dot_rows<T, DP, true, 4>(s0, qt, 0, k, p0, gt, 0, v, lane);
+      dot_rows<T, DP, true, 4, BESIDE>(s1, qt, 32, k, p1, gt, 32, v, lane);
+      weights(s0, p0, 0);
+      dot_cols<T, DP>(dv, gt, 0, s0, lane);
+      dot_cols<T, DP>(dk, qt, 0, p0, lane);
+      __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+#pragma unroll
+      for (int i = 0; i < DP / 8; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x2, BESIDE, 0);
+      }
+      weights(s1, p1, 32);
+      dot_cols<T, DP>(dv, gt, 32, s1, lane);
+      dot_cols<T, DP>(dk, qt, 32, p1, lane);
+      __builtin_amdgcn_sched_group_barrier(0x8, DP / 8, 0);
+    } else {
+#pragma unroll UNROLL
+      for (int qb = 0; qb < QB; ++qb) {
+        if (DP * sizeof(T) <= 128 && r0 + 32 * (block + qb) >= stop) break;
+        f32x16 s, dp;
+        dot_rows<T, DP, true, 4>(s, qt, 32 * (block + qb), k, dp, gt, 32 * (block + qb), v, lane);
+        weights(s, dp, 32 * (block + qb));
+        dot_cols<T, DP>(dv, gt, 32 * (block + qb), s, lane);
+        dot_cols<T, DP>(dk, qt, 32 * (block + qb), dp, lane);
+      }
     }
-  }
+  };
+  int buf = 0;
+  for (int r0 = beg; r0 < end; r0 += TR, buf = (buf + 1) % STAGES) step(buf, r0);
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   // an invisible key's columns hold what its zeros gave: nothing of it is stored
   if (!seen) { clear(dk); clear(dv); }
