@@ -281,7 +281,7 @@ __device__ __forceinline__ T* at(const void* base, const vf_attn_layout& l, int 
 template <typename T, int DP, int SW, bool GROUPED>
 struct Source {
   static constexpr int N = Ring<T, DP, SW>::N, CH = Ring<T, DP, SW>::CH, TR = Ring<T, DP, SW>::TR, WORDS = (TR + 63) / 64;
-  static_assert(64 % (NT / CH) == 0, "rows of a load within one word of bits");
+  static_assert(WORDS <= 2, "words of bits");
   const char* base;             // head 0 of row 0
   int64_t row_b, head_b;        // strides in bytes
   bool near;
@@ -326,8 +326,14 @@ struct Source {
         const RowOf ro = GROUPED ? row_of(j, r0 + row(i)) : RowOf{r0 + row(i), 0};
         p = base + ro.t * row_b + ro.g * head_b + off[i];
       }
-      const uint64_t mine = rows[i * (NT / CH) / 64] >> (threadIdx.x / CH);
-      lds_load16(((mine >> (i * (NT / CH) % 64)) & (head >> i) & 1) ? p : zeros, tile + i * (NT * 16));
+      uint64_t wanted;
+      if constexpr (NT % CH == 0) {                         // (a load's rows lie within one word)
+        wanted = rows[i * (NT / CH) / 64] >> (threadIdx.x / CH) >> (i * (NT / CH) % 64);
+      } else {
+        const int r = row(i);
+        wanted = (WORDS > 1 && r >= 64 ? rows[WORDS - 1] : rows[0]) >> (r & 63);
+      }
+      lds_load16((wanted & (head >> i) & 1) ? p : zeros, tile + i * (NT * 16));
     }
   }
 };
@@ -642,7 +648,8 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 256 ? 2 : 1) void xattn_fwd_k
 // rowsum(dO o) from the rounded o is off by e, and every dz by -p e: their sum, which should be 0, is -e.  The kernel behind is
 // given the exact rowsum.  Here dq is off by -scale e sum(p k): nothing beside the rounding of dz when many keys share a
 // row and o is small, but a third of the error at 77 keys (0.0027 of the norm, 0.0023 without it).  EXACT takes sum(p k) along and
-// removes it.
+// removes it; for sources of up to 2048 keys (heads of more than 96 elements, where its registers cost the second wavefront of a
+// SIMD: 512), not in parts.
 template <typename T, int DP, int SW, bool EXACT>
 __global__ __launch_bounds__(NT, DP * sizeof(T) * (EXACT ? 2 : 1) <= 256 ? 2 : 1) void xattn_dq_kernel(AttnJob j, AttnSplit sp) {
   using R = Ring<T, DP, SW>;
@@ -1023,43 +1030,50 @@ __global__ __launch_bounds__(NT) void xattn_join_kernel(AttnJob j, AttnSplit sp,
   }
 }
 
-// How the streamed side is split.  First among the wavefronts of a workgroup (sw): with 32 held rows to a workgroup instead of 128
-// there are four times as many workgroups and each goes through a quarter of the tiles' blocks, as long as that leaves at most
-// kFew workgroups.  Then into parts: one where the workgroups fill the compute units or the streamed tiles are few; else as
-// many as give every unit two workgroups.  Joining the parts costs a launch and a pass over fp32 partial results, about
-// 8 us, a streamed tile 1.2 us (bf16) or 2.5 (fp32): fewer than 8 (4) tiles saved do not pay.
-constexpr int kUnits = 256, kMaxParts = 64, kFew = 512;
-AttnSplit split_of(int64_t problems, int held, int streamed, int tile_rows, int most_sw, bool wide_tile) {
-  AttnSplit sp{};
-  sp.sw = 1;
-  for (int sw = 2; sw <= most_sw; sw *= 2)
-    if (problems * ((held + 128 / sw - 1) / (128 / sw)) <= kFew) sp.sw = sw;
-  const int block = 128 / sp.sw, least_saved = wide_tile ? 8 : 4;
-  tile_rows = std::max(tile_rows, 32 * sp.sw);
-  sp.tiles = (held + block - 1) / block;
-  const int all = std::max(1, (streamed + tile_rows - 1) / tile_rows);
-  const int64_t groups = problems * sp.tiles;
-  sp.per = all;
-  if (groups > 0 && groups < kUnits) {
-    const int parts = (int)std::min<int64_t>({(2 * kUnits + groups - 1) / groups, (int64_t)all, (int64_t)kMaxParts});
-    const int per = (all + parts - 1) / parts;
-    if (all - per >= least_saved) sp.per = per;
+// How the streamed side is split: among the wavefronts of a workgroup (sw: 128 / sw held rows to a workgroup, every wavefront a
+// quarter or half of a tile's blocks), and into parts, whose results a kernel behind joins.  Both make more and shorter workgroups
+// where few rows are held.  The choice is the one with the least estimated time, in us:
+//   a workgroup alone takes kStart + tiles * chain (its steps wait for each other), and as many of them run side by side as LDS and
+//   registers allow (`beside` to a compute unit);  workgroups of one compute unit share its matrix units: tiles * busy each.
+//   Parts cost kJoin and a pass over their fp32 results.
+// Measured per tile (forward): bf16 heads of 64: 1.1 chain, 0.55 busy (one block of 32 rows to a wavefront instead of two: 0.75, 0.3),
+// of 128: 1.8 and 1.15; fp32, bound by its matrix instructions: 2.4 and 2.1 at 64.  (192 workgroups of 7 tiles in three parts: 12.6 us
+// became 11.8 + 8.4; 256 workgroups of 24 tiles with sw = 4 instead of 1: 30 us became 19.)
+constexpr int kUnits = 256, kMaxParts = 64;
+constexpr float kStart = 5.f, kJoin = 8.f;
+AttnSplit split_of(const vf_attn_shape& s, int held, int streamed, float work) {
+  const bool b = s.dtype == VF_BF16;
+  const int dp = s.d_head <= 64 ? 64 : s.d_head <= 96 ? 96 : 128, problems = s.batch * s.kv_heads;
+  const int most = b || dp <= 64 ? 4 : 2;                   // (wider fp32 tiles for four wavefronts would not fit the LDS)
+  AttnSplit best{};
+  float least = 0.f;
+  for (int sw = 1; sw <= most; sw *= 2) {
+    const int block = 128 / sw, rows = std::max(b ? Elem<bf16_t>::TR : Elem<float>::TR, 32 * sw);
+    const bool two = rows / 32 / sw == 2;                   // blocks of a wavefront
+    const float wide = work * (float)dp / 64.f, chain = b ? (two ? 0.75f : 0.5f) + (two ? 0.35f : 0.25f) * wide : 0.3f + 2.1f * wide;
+    const float busy = b ? (two ? 0.55f : 0.3f) * wide : 2.1f * wide;
+    const int tile_bytes = rows * dp * (b ? 2 : 4), lds = (tile_bytes <= 8192 ? 6 : 4) * tile_bytes;
+    const int beside = std::max(1, std::min(b ? (dp <= 64 ? 3 : 2) : (dp <= 64 ? 2 : 1), 160 * 1024 / lds));
+    const int tiles = std::max(1, (held + block - 1) / block), all = std::max(1, (streamed + rows - 1) / rows);
+    const int64_t groups = std::max<int64_t>(1, (int64_t)problems * tiles);
+    for (int m = 0; m <= 4; ++m) {                          // one part, or as many as give every compute unit m workgroups
+      const int parts = m == 0 ? 1 : (int)std::min<int64_t>({(int64_t)kUnits * m / groups, (int64_t)all, (int64_t)kMaxParts});
+      if (parts < 1 || (m > 0 && parts == 1)) continue;
+      const int per = (all + parts - 1) / parts, n = (all + per - 1) / per;
+      const int64_t wgs = groups * n, rounds = (wgs + kUnits * beside - 1) / (kUnits * beside), load = (wgs + kUnits - 1) / kUnits;
+      float t = std::max((float)rounds * (kStart + (float)per * chain), kStart + (float)load * (float)per * busy);
+      if (n > 1) t += kJoin + (float)n * (float)problems * (float)held * (float)s.d_head * 2e-6f;
+      if (best.sw == 0 || t < least) {
+        least = t;
+        best.sw = sw; best.tiles = (held + block - 1) / block; best.parts = n; best.per = per;
+      }
+    }
   }
-  sp.parts = (all + sp.per - 1) / sp.per;
-  return sp;
+  return best;
 }
-// fp32 heads of more than 64 elements: tiles for four wavefronts would not fit the LDS.
-int most_sw(const vf_attn_shape& s) { return s.dtype == VF_BF16 || s.d_head <= 64 ? 4 : 2; }
 // The splits of the forward and dq kernels, and of the dk/dv kernel.
-AttnSplit split_rows(const vf_attn_shape& s) {
-  const bool b = s.dtype == VF_BF16;
-  return split_of((int64_t)s.batch * s.kv_heads, s.q_heads / s.kv_heads * s.q_rows, s.k_rows, b ? Elem<bf16_t>::TR : Elem<float>::TR,
-                  most_sw(s), b);
-}
-AttnSplit split_keys(const vf_attn_shape& s) {
-  const bool b = s.dtype == VF_BF16;
-  return split_of((int64_t)s.batch * s.kv_heads, s.k_rows, s.q_heads / s.kv_heads * s.q_rows, b ? Elem<bf16_t>::TR : Elem<float>::TR, most_sw(s), b);
-}
+AttnSplit split_rows(const vf_attn_shape& s) { return split_of(s, s.q_heads / s.kv_heads * s.q_rows, s.k_rows, 1.f); }
+AttnSplit split_keys(const vf_attn_shape& s) { return split_of(s, s.k_rows, s.q_heads / s.kv_heads * s.q_rows, 2.f); }
 int64_t round4(int64_t floats) { return (floats + 3) & ~int64_t(3); }
 // Floats of the parts of a pass over the rows (results and two statistics a row), and over the keys (dk and dv).
 int64_t part_rows_floats(const vf_attn_shape& s, const AttnSplit& sp) {
@@ -1096,7 +1110,6 @@ int launch_fwd(const AttnJob& j, const AttnSplit& sp, hipStream_t st) {
   VF_LAUNCH_CHECK();
   return VF_OK;
 }
-constexpr int kExactKeys = 512;
 template <typename T, int DP, int SW, bool EXACT>
 int launch_dq_of(const AttnJob& j, const AttnSplit& sp, hipStream_t st) {
   constexpr int lds = std::max(Ring<T, DP, SW>::LDS + kMaskWords * 8, Ring<T, DP, SW>::JOIN);
@@ -1108,9 +1121,10 @@ int launch_dq_of(const AttnJob& j, const AttnSplit& sp, hipStream_t st) {
 }
 template <typename T, int DP, int SW>
 int launch_dq(const AttnJob& j, const AttnSplit& sp, hipStream_t st) {
-  // (parts are made of more keys than that)
-  if constexpr (sizeof(T) == 2) return j.s.k_rows <= kExactKeys ? launch_dq_of<T, DP, SW, true>(j, sp, st) : launch_dq_of<T, DP, SW, false>(j, sp, st);
-  else return launch_dq_of<T, DP, SW, false>(j, sp, st);
+  if constexpr (sizeof(T) == 2) {
+    if (j.s.k_rows <= (DP <= 96 ? 2048 : 512) && sp.parts == 1) return launch_dq_of<T, DP, SW, true>(j, sp, st);
+  }
+  return launch_dq_of<T, DP, SW, false>(j, sp, st);
 }
 template <typename T, int DP, int SW>
 int launch_dkv(const AttnJob& j, const AttnSplit& sp, hipStream_t st) {
@@ -1160,6 +1174,13 @@ int launch_bwd(const AttnJob& j, float* ws, hipStream_t st) {
 
 }  // namespace
 
+// Heads are held and streamed in widths of 64, 96 and 128 elements, filled up with zeros.
+template <typename F>
+static int by_width(int d_head, F f) {
+  if (d_head <= 64) return f(std::integral_constant<int, 64>());
+  return d_head <= 96 ? f(std::integral_constant<int, 96>()) : f(std::integral_constant<int, 128>());
+}
+
 // The mask's bits; backward: two floats per row (lse and rowsum(dO o)); then the parts of one pass at a time.
 static int64_t mask_words(const vf_attn_shape& s) { return ((int64_t)s.k_rows + 63) / 64; }
 static int64_t mask_floats(const vf_attn_shape& s) { return round4(2 * s.batch * mask_words(s)); }
@@ -1188,9 +1209,8 @@ int launch_attn(AttnJob j, void* workspace, hipStream_t st) {
   float* ws = static_cast<float*>(workspace);
   VF_TRY(make_bits(j, ws, st));
   ws += mask_floats(j.s);
-  const bool wide = j.s.d_head > 64;
-  if (j.s.dtype == VF_BF16) return wide ? pass_rows<bf16_t, 128>(j, ws, false, st) : pass_rows<bf16_t, 64>(j, ws, false, st);
-  return wide ? pass_rows<float, 128>(j, ws, false, st) : pass_rows<float, 64>(j, ws, false, st);
+  if (j.s.dtype == VF_BF16) return by_width(j.s.d_head, [&](auto dp) { return pass_rows<bf16_t, decltype(dp)::value>(j, ws, false, st); });
+  return by_width(j.s.d_head, [&](auto dp) { return pass_rows<float, decltype(dp)::value>(j, ws, false, st); });
 }
 
 int launch_attn_bwd(AttnJob j, void* workspace, hipStream_t st) {
@@ -1201,9 +1221,8 @@ int launch_attn_bwd(AttnJob j, void* workspace, hipStream_t st) {
   j.row_lse = ws + mask_floats(j.s);
   j.row_delta = j.row_lse + rows;
   ws = j.row_delta + rows;
-  const bool wide = j.s.d_head > 64;
-  if (j.s.dtype == VF_BF16) return wide ? launch_bwd<bf16_t, 128>(j, ws, st) : launch_bwd<bf16_t, 64>(j, ws, st);
-  return wide ? launch_bwd<float, 128>(j, ws, st) : launch_bwd<float, 64>(j, ws, st);
+  if (j.s.dtype == VF_BF16) return by_width(j.s.d_head, [&](auto dp) { return launch_bwd<bf16_t, decltype(dp)::value>(j, ws, st); });
+  return by_width(j.s.d_head, [&](auto dp) { return launch_bwd<float, decltype(dp)::value>(j, ws, st); });
 }
 
 }  // namespace vf
