@@ -429,6 +429,14 @@ __device__ __forceinline__ void remove(f32x16 (&a)[N], const f32x16 (&b)[N], flo
 #pragma unroll
     for (int r = 0; r < 16; ++r) a[i][r] = fmaf(-f, b[i][r], a[i][r]);
 }
+// Wavefronts to a SIMD that the kernels' registers are kept down to: two wherever that spills nothing (next to nothing at
+// fp32 of 64 with four wavefronts to a block), else one.
+template <typename T, int DP> constexpr int fwd_waves() { return DP * sizeof(T) <= 384 ? 2 : 1; }
+template <typename T, int DP, int SW, bool EXACT> constexpr int dq_waves() {
+  return sizeof(T) == 4 ? (DP <= 64 ? 2 : 1) : !EXACT || DP <= 64 || (DP <= 96 && SW < 4) ? 2 : 1;
+}
+template <typename T, int DP> constexpr int dkv_waves() { return DP * sizeof(T) <= 128 ? 2 : 1; }
+
 // Row r of the problem in part w.part's partial results.
 __device__ __forceinline__ int64_t part_row(const AttnJob& j, const Problem& p, const Work& w, int r) {
   return ((int64_t)w.part * j.s.batch * j.s.kv_heads + w.id) * p.rows + r;
@@ -469,7 +477,7 @@ __device__ __forceinline__ void join_queries(const AttnJob& j, const Problem& p,
 
 // ---- forward ------------------------------------------------------------------------------------
 template <typename T, int DP, int SW>
-__global__ __launch_bounds__(NT, DP * sizeof(T) <= 256 ? 2 : 1) void xattn_fwd_kernel(AttnJob j, AttnSplit sp) {
+__global__ __launch_bounds__(NT, (fwd_waves<T, DP>())) void xattn_fwd_kernel(AttnJob j, AttnSplit sp) {
   using R = Ring<T, DP, SW>;
   constexpr int TR = R::TR, KB = TR / 32 / SW, RW = 4 / SW, ELEMS = R::ELEMS, STAGES = R::STAGES, BYTES = R::BYTES;
   constexpr int WORDS = Source<T, DP, SW, false>::WORDS;
@@ -490,6 +498,7 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 256 ? 2 : 1) void xattn_fwd_k
   const float c = j.s.scale * kLog2e;
 
   Held<T, DP> q;
+  q.load(live ? at<const T>(j.q, j.s.q, p.b, ro.t, head) : nullptr, dh, half);
   f32x16 o[DP / 32];
   clear(o);
   float m = -INFINITY, l = 0.f, ref = 0.f, base = 0.f;
@@ -517,7 +526,6 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 256 ? 2 : 1) void xattn_fwd_k
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) issue(kbeg + i * TR, i);
   }
-  q.load(live ? at<const T>(j.q, j.s.q, p.b, ro.t, head) : nullptr, dh, half);
   q.arrive();
   auto step = [&](auto buf, int k0) {
     const T* kt = lds + buf * 2 * ELEMS;
@@ -651,7 +659,7 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) <= 256 ? 2 : 1) void xattn_fwd_k
 // removes it; for sources of up to 2048 keys (heads of more than 96 elements, where its registers cost the second wavefront of a
 // SIMD: 512), not in parts.
 template <typename T, int DP, int SW, bool EXACT>
-__global__ __launch_bounds__(NT, DP * sizeof(T) * (EXACT ? 2 : 1) <= 256 ? 2 : 1) void xattn_dq_kernel(AttnJob j, AttnSplit sp) {
+__global__ __launch_bounds__(NT, (dq_waves<T, DP, SW, EXACT>())) void xattn_dq_kernel(AttnJob j, AttnSplit sp) {
   using R = Ring<T, DP, SW>;
   constexpr int TR = R::TR, KB = TR / 32 / SW, RW = 4 / SW, ELEMS = R::ELEMS, STAGES = R::STAGES, BYTES = R::BYTES;
   constexpr int WORDS = Source<T, DP, SW, false>::WORDS;
@@ -805,7 +813,7 @@ __global__ __launch_bounds__(NT, DP * sizeof(T) * (EXACT ? 2 : 1) <= 256 ? 2 : 1
 
 // ---- backward: dk and dv ------------------------------------------------------------------------------
 template <typename T, int DP, int SW>
-__global__ __launch_bounds__(NT, DP * sizeof(T) <= 128 ? 2 : 1) void xattn_dkv_kernel(AttnJob j, AttnSplit sp) {
+__global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void xattn_dkv_kernel(AttnJob j, AttnSplit sp) {
   using R = Ring<T, DP, SW>;
   constexpr int TR = R::TR, QB = TR / 32 / SW, RW = 4 / SW, ELEMS = R::ELEMS, STAGES = R::STAGES, BYTES = R::BYTES;
   constexpr int WORDS = Source<T, DP, SW, false>::WORDS, STAT = 64 * WORDS;   // rows of statistics of a stage
@@ -1053,7 +1061,7 @@ AttnSplit split_of(const vf_attn_shape& s, int held, int streamed, float work) {
     const float wide = work * (float)dp / 64.f, chain = b ? (two ? 0.75f : 0.5f) + (two ? 0.35f : 0.25f) * wide : 0.3f + 2.1f * wide;
     const float busy = b ? (two ? 0.55f : 0.3f) * wide : 2.1f * wide;
     const int tile_bytes = rows * dp * (b ? 2 : 4), lds = (tile_bytes <= 8192 ? 6 : 4) * tile_bytes;
-    const int beside = std::max(1, std::min(b ? (dp <= 64 ? 3 : 2) : (dp <= 64 ? 2 : 1), 160 * 1024 / lds));
+    const int beside = std::max(1, std::min(b ? (dp <= 64 ? 3 : 2) : (dp <= 96 ? 2 : 1), 160 * 1024 / lds));
     const int tiles = std::max(1, (held + block - 1) / block), all = std::max(1, (streamed + rows - 1) / rows);
     const int64_t groups = std::max<int64_t>(1, (int64_t)problems * tiles);
     for (int m = 0; m <= 4; ++m) {                          // one part, or as many as give every compute unit m workgroups
