@@ -346,7 +346,8 @@ int vf_gemm_noalloc(const void* A, int64_t lda, const void* B, int64_t ldb, floa
  * Conventions of these entry points, beside those at the top of this file
  *   - a tensor [rows, heads, d_head] or [batch, rows, heads, d_head] is given by a pointer and its
  *     strides in ELEMENTS; the elements of a head are contiguous.  Input strides may be any (0 repeats
- *     a row or head), output strides must keep the outputs apart;
+ *     a row or head), output strides must keep the outputs apart; outputs overlap no input except
+ *     where a call says so;
  *   - device memory is on the current device; work is enqueued on `stream` (NULL = the default
  *     stream), nothing is allocated, nothing synchronises, and no state is kept between calls, so
  *     calls on different streams do not disturb each other as long as each has its own workspace.
@@ -389,7 +390,7 @@ int vf_rope_make(int32_t layout, int32_t rot_dim, double base, int32_t scaling, 
  * t = 2 pi p turns[j] (reduced in float64: exact for far positions) and the plan's scale s;
  * elements from rot_dim on are copied.  inverse != 0 turns by -t: with the same scale that is the
  * operator's backward pass (dx from dy).  positions: device int32 [rows], or NULL for
- * first + (seq_len > 0 ? row % seq_len : row).  d_head: rot_dim .. 512.  y may be x (same strides). */
+ * first + (seq_len > 0 ? row % seq_len : row).  d_head: rot_dim .. 512, heads: up to 8192.  y may be x (same strides). */
 int vf_rope(int32_t dtype, const void* x, int64_t x_row, int64_t x_head, void* y, int64_t y_row,
             int64_t y_head, int64_t rows, int32_t heads, int32_t d_head, const int32_t* positions,
             int64_t first, int64_t seq_len, const vf_rope_plan* plan, int32_t inverse, void* stream);

@@ -1062,6 +1062,7 @@ AttnSplit split_of(const vf_attn_shape& s, int held, int streamed, float work) {
     const float busy = b ? (two ? 0.55f : 0.3f) * wide : 2.1f * wide;
     const int tile_bytes = rows * dp * (b ? 2 : 4), lds = (tile_bytes <= 8192 ? 6 : 4) * tile_bytes;
     const int beside = std::max(1, std::min(b ? (dp <= 64 ? 3 : 2) : (dp <= 96 ? 2 : 1), 160 * 1024 / lds));
+    if (sw > 1 && (held + block - 1) / block > 65535) break;    // (a dimension of the grid)
     const int tiles = std::max(1, (held + block - 1) / block), all = std::max(1, (streamed + rows - 1) / rows);
     const int64_t groups = std::max<int64_t>(1, (int64_t)problems * tiles);
     for (int m = 0; m <= 4; ++m) {                          // one part, or as many as give every compute unit m workgroups

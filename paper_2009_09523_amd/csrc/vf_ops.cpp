@@ -11,7 +11,7 @@ using namespace vf;
 namespace {
 
 constexpr int64_t kMaxRows = INT32_MAX;
-constexpr int kMaxHeads = 65535, kMaxHead = 512;
+constexpr int kMaxHeads = 8192, kMaxHead = 512;            // (heads: an item's row is found by a multiplication that is exact up to there)
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 

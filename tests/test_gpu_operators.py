@@ -382,6 +382,11 @@ SHAPES = [  # batch, q rows, k rows, q heads, kv heads, d_head
     (1, 1, 1, 1, 1, 64), (2, 1, 300, 2, 2, 64), (1, 1, 700, 8, 2, 128), (3, 5, 33, 2, 1, 32), (2, 33, 31, 3, 3, 40),
     (1, 128, 128, 2, 2, 64), (2, 129, 65, 2, 1, 128), (1, 200, 77, 4, 4, 80), (1, 63, 513, 3, 1, 96), (2, 7, 1, 4, 2, 8),
     (1, 300, 3, 5, 1, 120), (1, 257, 260, 6, 2, 64), (1, 1, 2500, 4, 1, 64), (1, 1030, 9, 2, 2, 64), (2, 4, 1111, 2, 2, 128),
+    # many workgroups: rows, then keys, in tiles of 128 to a workgroup, every width
+    (16, 260, 90, 8, 8, 64), (16, 260, 90, 8, 8, 96), (16, 260, 90, 8, 8, 128), (12, 90, 400, 8, 4, 64), (12, 90, 400, 8, 8, 80),
+    (12, 90, 400, 8, 8, 104),
+    # few: the streamed side in parts
+    (1, 1, 20000, 1, 1, 64), (1, 2, 9000, 4, 2, 128), (1, 3000, 20, 2, 1, 128), (1, 40, 6000, 2, 2, 96), (1, 4000, 40, 2, 1, 96),
 ]
 
 
