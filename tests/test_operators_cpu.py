@@ -57,15 +57,19 @@ def _rope(**kw):
     a = dict(dtype=1, x=P, x_row=256, x_head=64, y=2 * P, y_row=256, y_head=64, rows=8, heads=4, dh=64, positions=None, first=0, seq_len=0,
              plan=vf.vf_rope_make(0, 64), inverse=0) | kw
     plan = a.pop("plan")
+    plan = plan() if callable(plan) else plan
     v = list(a.values())
     return vf.lib().vf_rope(*v[:13], C.byref(plan) if plan is not None else None, v[13], None)
 
 
 def _bad_plan(**kw):
-    p = vf.vf_rope_make(0, 64)
-    for k, v in kw.items():
-        setattr(p, k, v)
-    return p
+    """A plan with fields set wrong, made when it is called for (nothing here loads the library at import)."""
+    def make():
+        p = vf.vf_rope_make(0, 64)
+        for k, v in kw.items():
+            setattr(p, k, v)
+        return p
+    return make
 
 
 @pytest.mark.parametrize("kw", [dict(dtype=2), dict(x=None), dict(y=None), dict(x=P + 1), dict(y=P + 1), dict(rows=-1), dict(rows=1 << 31),
@@ -90,7 +94,8 @@ def _norm(backward=False, **kw):
     if backward:
         a |= dict(dgq=None, dgk=None, alpha=1.0, accumulate=0, ws=None, ws_bytes=0)
     a |= kw
-    a["plan"] = C.byref(a["plan"]) if a["plan"] is not None else None
+    plan = a["plan"]() if callable(a["plan"]) else a["plan"]
+    a["plan"] = C.byref(plan) if plan is not None else None
     f = vf.lib().vf_qk_norm_rope_backward if backward else vf.lib().vf_qk_norm_rope
     return f(*a.values(), None)
 
