@@ -236,42 +236,59 @@ def vf_gemm_noalloc(A, B, Cout, M: int, N: int, K: int, alpha: float = 1.0, accu
 
 
 # These calls are made many times a step on tensors that may be small, so the checks are written to cost little: a call
-# spends 3 to 6 us here and in ctypes beside the 3 to 4 us of a kernel launch.
+# spends 2 to 4 us here and in ctypes beside the 3 to 4 us of a kernel launch.
 
 
 def _refuse(where: str, why: str):
     raise VfError(VF_EINVAL, where, why)
 
 
-def _device_of(where: str, t) -> int:
-    """The current device, on which the first operand has to be (the others are held against it)."""
-    import torch
-    dev = t.get_device()
-    if dev < 0 or dev != torch.cuda.current_device():
-        _refuse(where, f"a tensor is on {t.device}, not on the current device")
-    return dev
+class _Torch:
+    """What the checks ask of torch, taken once (the module itself does not import torch)."""
+
+    def __init__(self):
+        import torch
+        self.f32, self.i32, self.u8, self.bool = torch.float32, torch.int32, torch.uint8, torch.bool
+        self.codes = {torch.bfloat16: VF_BF16, torch.float32: VF_F32}
+        self.current = torch.cuda.current_device
+        self.alone = torch.cuda.is_available() and torch.cuda.device_count() == 1   # one device: it is the current one
 
 
-def _operand(where: str, t, like, dev: int):
-    """Strides of a floating operand of `like`'s type with contiguous heads."""
-    if t.get_device() != dev:
-        _refuse(where, f"a tensor is on {t.device}, not on the current device")
-    if t.dtype is not like.dtype:
-        _refuse(where, f"tensors of {t.dtype} and {like.dtype}")
-    s = t.stride()
-    if not s or s[-1] != 1 and t.shape[-1] > 1:
-        _refuse(where, "the elements of a head are not contiguous")
-    return s
+_torch_facts = None
+
+
+def _facts() -> _Torch:
+    global _torch_facts
+    if _torch_facts is None:
+        _torch_facts = _Torch()
+    return _torch_facts
+
+
+def _floats(where: str, *tensors):
+    """(facts, device, type code, strides...) of floating operands: one type, on the current device, heads contiguous."""
+    t = _torch_facts or _facts()
+    first = tensors[0]
+    dev, dtype = first.get_device(), first.dtype
+    code = t.codes.get(dtype)
+    if code is None:
+        _refuse(where, f"tensors of {dtype}")
+    if dev < 0 or not (t.alone or dev == t.current()):
+        _refuse(where, f"a tensor is on {first.device}, not on the current device")
+    out = [t, dev, code]
+    for x in tensors:
+        s = x.stride()
+        if x.get_device() != dev or x.dtype is not dtype or not s or (s[-1] != 1 and x.shape[-1] > 1):
+            _refuse(where, f"a tensor of {x.dtype} on {x.device} with strides {s}: operands are {dtype} on {first.device}, elements of a head contiguous")
+        out.append(s)
+    return out
 
 
 def _side(where: str, t, dev: int, shape, dtype):
     """Address of a contiguous side tensor (positions, weights, lengths, statistics) or None."""
     if t is None:
         return None
-    if t.get_device() != dev:
-        _refuse(where, f"a tensor is on {t.device}, not on the current device")
-    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
-        _refuse(where, f"expected a contiguous {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    if t.get_device() != dev or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        _refuse(where, f"expected a contiguous {dtype} tensor of shape {tuple(shape)} on device {dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
@@ -282,15 +299,6 @@ def _space(where: str, t, dev: int):
     if t.get_device() != dev or not t.is_contiguous():
         _refuse(where, "the workspace is not a contiguous tensor on the current device")
     return t.data_ptr(), t.numel() * t.element_size()
-
-
-def _float_code(where: str, t) -> int:
-    import torch
-    if t.dtype is torch.bfloat16:
-        return VF_BF16
-    if t.dtype is torch.float32:
-        return VF_F32
-    _refuse(where, f"tensors of {t.dtype}")
 
 
 def vf_rope_make(layout: int, rot_dim: int, base: float = 10000.0, scaling: int = VF_ROPE_PLAIN, factor: float = 1.0,
@@ -305,16 +313,15 @@ def vf_rope_make(layout: int, rot_dim: int, base: float = 10000.0, scaling: int 
 def vf_rope(x, y, plan: VfRopePlan, positions=None, first: int = 0, seq_len: int = 0, inverse: bool = False, stream=None):
     """y = x with the heads turned by their rows' positions (inverse: the backward pass).  x, y: [rows, heads, d_head]
     of any row and head strides; y may be x.  positions: int32 [rows], or None: first + row (% seq_len)."""
-    import torch
     where = "vf_rope"
-    dev = _device_of(where, x)
-    xs, ys, shape = _operand(where, x, x, dev), _operand(where, y, x, dev), x.shape
+    t, dev, code, xs, ys = _floats(where, x, y)
+    shape = x.shape
     if len(shape) != 3 or y.shape != shape:
         _refuse(where, "x and y are [rows, heads, d_head]")
     rows, heads, dh = shape
-    rc = lib().vf_rope(_float_code(where, x), x.data_ptr(), xs[0], xs[1], y.data_ptr(), ys[0], ys[1], rows, heads, dh,
-                       _side(where, positions, dev, (rows,), torch.int32), first, seq_len, C.byref(plan), bool(inverse),
-                       _stream_handle(stream))
+    rc = lib().vf_rope(code, x.data_ptr(), xs[0], xs[1], y.data_ptr(), ys[0], ys[1], rows, heads, dh,
+                       None if positions is None else _side(where, positions, dev, (rows,), t.i32), first, seq_len, C.byref(plan),
+                       bool(inverse), None if stream is None else stream.cuda_stream)
     if rc:
         _check(rc, where)
 
@@ -323,18 +330,16 @@ def vf_qk_norm_rope(x, y, q_heads: int, gamma_q=None, gamma_k=None, eps: float =
                     positions=None, first: int = 0, seq_len: int = 0, stream=None):
     """RMS norm of every head (weights gamma_q for the first q_heads heads, gamma_k for the others; None: ones) and, with a
     plan, the rotation.  x, y: [rows, heads, d_head]; y may be x."""
-    import torch
     where = "vf_qk_norm_rope"
-    dev = _device_of(where, x)
-    xs, ys, shape = _operand(where, x, x, dev), _operand(where, y, x, dev), x.shape
+    t, dev, code, xs, ys = _floats(where, x, y)
+    shape = x.shape
     if len(shape) != 3 or y.shape != shape:
         _refuse(where, "x and y are [rows, heads, d_head]")
     rows, heads, dh = shape
-    f32 = torch.float32
-    rc = lib().vf_qk_norm_rope(_float_code(where, x), x.data_ptr(), xs[0], xs[1], y.data_ptr(), ys[0], ys[1], rows, q_heads,
-                               heads - q_heads, dh, _side(where, gamma_q, dev, (dh,), f32), _side(where, gamma_k, dev, (dh,), f32),
-                               eps, _side(where, positions, dev, (rows,), torch.int32), first, seq_len,
-                               C.byref(plan) if plan is not None else None, _stream_handle(stream))
+    rc = lib().vf_qk_norm_rope(code, x.data_ptr(), xs[0], xs[1], y.data_ptr(), ys[0], ys[1], rows, q_heads, heads - q_heads, dh,
+                               _side(where, gamma_q, dev, (dh,), t.f32), _side(where, gamma_k, dev, (dh,), t.f32), eps,
+                               _side(where, positions, dev, (rows,), t.i32), first, seq_len,
+                               None if plan is None else C.byref(plan), None if stream is None else stream.cuda_stream)
     if rc:
         _check(rc, where)
 
@@ -351,21 +356,20 @@ def vf_qk_norm_rope_backward(x, dy, dx, q_heads: int, gamma_q=None, gamma_k=None
                              eps: float = 1e-6, plan: Optional[VfRopePlan] = None, positions=None, first: int = 0,
                              seq_len: int = 0, alpha: float = 1.0, accumulate: bool = False, stream=None):
     """dx from dy (dx may be x or dy); dgamma = alpha * its sum over rows and heads (+ dgamma if accumulate)."""
-    import torch
     where = "vf_qk_norm_rope_backward"
-    dev = _device_of(where, x)
-    xs, gs, ds, shape = _operand(where, x, x, dev), _operand(where, dy, x, dev), _operand(where, dx, x, dev), x.shape
+    t, dev, code, xs, gs, ds = _floats(where, x, dy, dx)
+    shape = x.shape
     if len(shape) != 3 or dy.shape != shape or dx.shape != shape:
         _refuse(where, "x, dy and dx are [rows, heads, d_head]")
     rows, heads, dh = shape
-    f32, one = torch.float32, (dh,)
+    f32, one = t.f32, (dh,)
     ws, size = _space(where, workspace, dev)
     rc = lib().vf_qk_norm_rope_backward(
-        _float_code(where, x), x.data_ptr(), xs[0], xs[1], dy.data_ptr(), gs[0], gs[1], dx.data_ptr(), ds[0], ds[1], rows,
+        code, x.data_ptr(), xs[0], xs[1], dy.data_ptr(), gs[0], gs[1], dx.data_ptr(), ds[0], ds[1], rows,
         q_heads, heads - q_heads, dh, _side(where, gamma_q, dev, one, f32), _side(where, gamma_k, dev, one, f32), eps,
-        _side(where, positions, dev, (rows,), torch.int32), first, seq_len, C.byref(plan) if plan is not None else None,
+        _side(where, positions, dev, (rows,), t.i32), first, seq_len, None if plan is None else C.byref(plan),
         _side(where, dgamma_q, dev, one, f32), _side(where, dgamma_k, dev, one, f32), alpha, bool(accumulate), ws, size,
-        _stream_handle(stream))
+        None if stream is None else stream.cuda_stream)
     if rc:
         _check(rc, where)
 
@@ -374,7 +378,7 @@ _ATTN_SHAPE = struct.Struct("=7if24q")       # vf_attn_shape, field for field
 _ATTN_NONE = (0,) * 12
 
 
-def _attn_sizes(where: str, q, k, v, scale):
+def _attn_sizes(where: str, code: int, q, k, v, scale):
     """(the fields of vf_attn_shape before the layouts)"""
     shape, ks = q.shape, k.shape
     if len(shape) != 4 or len(ks) != 4 or v.shape != ks:
@@ -384,23 +388,24 @@ def _attn_sizes(where: str, q, k, v, scale):
         _refuse(where, "q, k and v differ in batch or head size")
     if max(B, Tq, ks[1], Hq, ks[2], dh) > 0x7fffffff:
         _refuse(where, "a size is beyond 32 bits")
-    return _float_code(where, q), B, Tq, ks[1], Hq, ks[2], dh, dh ** -0.5 if scale is None else scale
+    return code, B, Tq, ks[1], Hq, ks[2], dh, dh ** -0.5 if scale is None else scale
 
 
-def _attn_masks(where: str, dev: int, B: int, Tk: int, q_len, k_len, key_mask):
+def _attn_masks(where: str, t: _Torch, dev: int, B: int, Tk: int, q_len, k_len, key_mask):
     if q_len is None and k_len is None and key_mask is None:
         return None, None, None
-    import torch
-    if key_mask is not None and key_mask.dtype is torch.bool:
-        key_mask = key_mask.view(torch.uint8)
-    return (_side(where, q_len, dev, (B,), torch.int32), _side(where, k_len, dev, (B,), torch.int32),
-            _side(where, key_mask, dev, (B, Tk), torch.uint8))
+    if key_mask is not None and key_mask.dtype is t.bool:
+        key_mask = key_mask.view(t.u8)
+    return (_side(where, q_len, dev, (B,), t.i32), _side(where, k_len, dev, (B,), t.i32), _side(where, key_mask, dev, (B, Tk), t.u8))
 
 
 def vf_attention_workspace(q, k, v, backward: bool = False) -> int:
     """Bytes of workspace the call over tensors of these shapes needs."""
     where = "vf_attention_workspace"
-    n = int(lib().vf_attention_workspace(_ATTN_SHAPE.pack(*_attn_sizes(where, q, k, v, 1.0), *_ATTN_NONE, *_ATTN_NONE), bool(backward)))
+    code = _facts().codes.get(q.dtype)
+    if code is None:
+        _refuse(where, f"tensors of {q.dtype}")
+    n = int(lib().vf_attention_workspace(_ATTN_SHAPE.pack(*_attn_sizes(where, code, q, k, v, 1.0), *_ATTN_NONE, *_ATTN_NONE), bool(backward)))
     if n < 0:
         _check(n, where)
     return n
@@ -410,17 +415,16 @@ def vf_attention(q, k, v, o, lse=None, q_len=None, k_len=None, key_mask=None, sc
     """o = softmax(scale q k^T) v over the visible keys.  q, o: [batch, q_rows, q_heads, d_head]; k, v: [batch, k_rows,
     kv_heads, d_head]; lse: fp32 [batch, q_heads, q_rows] for the backward pass; q_len, k_len: int32 [batch]; key_mask:
     uint8 or bool [batch, k_rows]; scale: 1 / sqrt(d_head) if None."""
-    import torch
     where = "vf_attention"
-    dev = _device_of(where, q)
-    lay = (*_operand(where, q, q, dev)[:3], *_operand(where, k, q, dev)[:3], *_operand(where, v, q, dev)[:3], *_operand(where, o, q, dev)[:3])
-    sizes = _attn_sizes(where, q, k, v, scale)
+    t, dev, code, qs, ks, vs, os_ = _floats(where, q, k, v, o)
+    sizes = _attn_sizes(where, code, q, k, v, scale)
     if o.shape != q.shape:
         _refuse(where, "o has the shape of q")
     ws, size = _space(where, workspace, dev)
-    rc = lib().vf_attention(_ATTN_SHAPE.pack(*sizes, *lay, *_ATTN_NONE), q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                            *_attn_masks(where, dev, sizes[1], sizes[3], q_len, k_len, key_mask), o.data_ptr(),
-                            _side(where, lse, dev, (sizes[1], sizes[4], sizes[2]), torch.float32), ws, size, _stream_handle(stream))
+    rc = lib().vf_attention(_ATTN_SHAPE.pack(*sizes, *qs[:3], *ks[:3], *vs[:3], *os_[:3], *_ATTN_NONE), q.data_ptr(), k.data_ptr(),
+                            v.data_ptr(), *_attn_masks(where, t, dev, sizes[1], sizes[3], q_len, k_len, key_mask), o.data_ptr(),
+                            _side(where, lse, dev, (sizes[1], sizes[4], sizes[2]), t.f32), ws, size,
+                            None if stream is None else stream.cuda_stream)
     if rc:
         _check(rc, where)
 
@@ -428,18 +432,16 @@ def vf_attention(q, k, v, o, lse=None, q_len=None, k_len=None, key_mask=None, sc
 def vf_attention_backward(q, k, v, o, lse, d_o, dq, dk, dv, q_len=None, k_len=None, key_mask=None, scale=None, workspace=None,
                           stream=None):
     """Gradients dq, dk, dv from d_o; o and lse as vf_attention wrote them, the same lengths, mask and scale."""
-    import torch
     where = "vf_attention_backward"
-    dev = _device_of(where, q)
-    lay = [x for t in (q, k, v, o, d_o, dq, dk, dv) for x in _operand(where, t, q, dev)[:3]]
-    sizes = _attn_sizes(where, q, k, v, scale)
+    t, dev, code, *lay = _floats(where, q, k, v, o, d_o, dq, dk, dv)
+    sizes = _attn_sizes(where, code, q, k, v, scale)
     if not q.shape == o.shape == d_o.shape == dq.shape or not k.shape == dk.shape == dv.shape:
         _refuse(where, "o, d_o and dq have the shape of q, dk and dv that of k")
     ws, size = _space(where, workspace, dev)
-    rc = lib().vf_attention_backward(_ATTN_SHAPE.pack(*sizes, *lay), q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                                     *_attn_masks(where, dev, sizes[1], sizes[3], q_len, k_len, key_mask), o.data_ptr(),
-                                     _side(where, lse, dev, (sizes[1], sizes[4], sizes[2]), torch.float32), d_o.data_ptr(),
-                                     dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ws, size, _stream_handle(stream))
+    rc = lib().vf_attention_backward(_ATTN_SHAPE.pack(*sizes, *[n for s in lay for n in s[:3]]), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                     *_attn_masks(where, t, dev, sizes[1], sizes[3], q_len, k_len, key_mask), o.data_ptr(),
+                                     _side(where, lse, dev, (sizes[1], sizes[4], sizes[2]), t.f32), d_o.data_ptr(),
+                                     dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ws, size, None if stream is None else stream.cuda_stream)
     if rc:
         _check(rc, where)
 
