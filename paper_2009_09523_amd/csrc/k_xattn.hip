@@ -1043,13 +1043,14 @@ __global__ __launch_bounds__(NT) void xattn_join_kernel(AttnJob j, AttnSplit sp,
 // where few rows are held.  The choice is the one with the least estimated time, in us:
 //   a workgroup alone takes kStart + tiles * chain (its steps wait for each other), and as many of them run side by side as LDS and
 //   registers allow (`beside` to a compute unit);  workgroups of one compute unit share its matrix units: tiles * busy each.
-//   Parts cost kJoin and a pass over their fp32 results.
+//   Joining the wavefronts' results takes 1 us for 64 elements, parts cost kJoin and a pass over their fp32 results.
 // Measured per tile (forward): bf16 heads of 64: 1.1 chain, 0.55 busy (one block of 32 rows to a wavefront instead of two: 0.75, 0.3),
 // of 128: 1.8 and 1.15; fp32, bound by its matrix instructions: 2.4 and 2.1 at 64.  (192 workgroups of 7 tiles in three parts: 12.6 us
-// became 11.8 + 8.4; 256 workgroups of 24 tiles with sw = 4 instead of 1: 30 us became 19.)
+// became 11.8 + 8.4; 256 workgroups of 24 tiles with sw = 4 instead of 1: 30 us became 19; 256 of 4 tiles, 128 wide: 13 us with
+// sw = 1, 15 with 2, 31 with 4.)
 constexpr int kUnits = 256, kMaxParts = 64;
 constexpr float kStart = 5.f, kJoin = 8.f;
-AttnSplit split_of(const vf_attn_shape& s, int held, int streamed, float work) {
+AttnSplit split_of(const vf_attn_shape& s, int held, int streamed, float work, bool alone) {
   const bool b = s.dtype == VF_BF16;
   const int dp = s.d_head <= 64 ? 64 : s.d_head <= 96 ? 96 : 128, problems = s.batch * s.kv_heads;
   const int most = b || dp <= 64 ? 4 : 2;                   // (wider fp32 tiles for four wavefronts would not fit the LDS)
@@ -1061,7 +1062,8 @@ AttnSplit split_of(const vf_attn_shape& s, int held, int streamed, float work) {
     const float wide = work * (float)dp / 64.f, chain = b ? (two ? 0.75f : 0.5f) + (two ? 0.35f : 0.25f) * wide : 0.3f + 2.1f * wide;
     const float busy = b ? (two ? 0.55f : 0.3f) * wide : 2.1f * wide;
     const int tile_bytes = rows * dp * (b ? 2 : 4), lds = (tile_bytes <= 8192 ? 6 : 4) * tile_bytes;
-    const int beside = std::max(1, std::min(b ? (dp <= 64 ? 3 : 2) : (dp <= 96 ? 2 : 1), 160 * 1024 / lds));
+    const int beside = alone ? 1 : std::max(1, std::min(b ? (dp <= 64 ? 3 : 2) : (dp <= 96 ? 2 : 1), 160 * 1024 / lds));
+    const float start = kStart + (sw > 1 ? (float)dp / 64.f : 0.f);
     if (sw > 1 && (held + block - 1) / block > 65535) break;    // (a dimension of the grid)
     const int tiles = std::max(1, (held + block - 1) / block), all = std::max(1, (streamed + rows - 1) / rows);
     const int64_t groups = std::max<int64_t>(1, (int64_t)problems * tiles);
@@ -1070,7 +1072,7 @@ AttnSplit split_of(const vf_attn_shape& s, int held, int streamed, float work) {
       if (parts < 1 || (m > 0 && parts == 1)) continue;
       const int per = (all + parts - 1) / parts, n = (all + per - 1) / per;
       const int64_t wgs = groups * n, rounds = (wgs + kUnits * beside - 1) / (kUnits * beside), load = (wgs + kUnits - 1) / kUnits;
-      float t = std::max((float)rounds * (kStart + (float)per * chain), kStart + (float)load * (float)per * busy);
+      float t = std::max((float)rounds * (start + (float)per * chain), start + (float)load * (float)per * busy);
       if (n > 1) t += kJoin + (float)n * (float)problems * (float)held * (float)s.d_head * 2e-6f;
       if (best.sw == 0 || t < least) {
         least = t;
@@ -1080,9 +1082,13 @@ AttnSplit split_of(const vf_attn_shape& s, int held, int streamed, float work) {
   }
   return best;
 }
+// Sources for which dq takes sum(p k) along (see its kernel): above 96 elements that leaves one workgroup to a compute unit.
+bool exact_dq(const vf_attn_shape& s) { return s.dtype == VF_BF16 && s.k_rows <= (s.d_head <= 96 ? 2048 : 512); }
 // The splits of the forward and dq kernels, and of the dk/dv kernel.
-AttnSplit split_rows(const vf_attn_shape& s) { return split_of(s, s.q_heads / s.kv_heads * s.q_rows, s.k_rows, 1.f); }
-AttnSplit split_keys(const vf_attn_shape& s) { return split_of(s, s.k_rows, s.q_heads / s.kv_heads * s.q_rows, 2.f); }
+AttnSplit split_rows(const vf_attn_shape& s, bool backward) {
+  return split_of(s, s.q_heads / s.kv_heads * s.q_rows, s.k_rows, 1.f, backward && s.d_head > 96 && exact_dq(s));
+}
+AttnSplit split_keys(const vf_attn_shape& s) { return split_of(s, s.k_rows, s.q_heads / s.kv_heads * s.q_rows, 2.f, false); }
 int64_t round4(int64_t floats) { return (floats + 3) & ~int64_t(3); }
 // Floats of the parts of a pass over the rows (results and two statistics a row), and over the keys (dk and dv).
 int64_t part_rows_floats(const vf_attn_shape& s, const AttnSplit& sp) {
@@ -1131,7 +1137,7 @@ int launch_dq_of(const AttnJob& j, const AttnSplit& sp, hipStream_t st) {
 template <typename T, int DP, int SW>
 int launch_dq(const AttnJob& j, const AttnSplit& sp, hipStream_t st) {
   if constexpr (sizeof(T) == 2) {
-    if (j.s.k_rows <= (DP <= 96 ? 2048 : 512) && sp.parts == 1) return launch_dq_of<T, DP, SW, true>(j, sp, st);
+    if (exact_dq(j.s) && sp.parts == 1) return launch_dq_of<T, DP, SW, true>(j, sp, st);
   }
   return launch_dq_of<T, DP, SW, false>(j, sp, st);
 }
@@ -1150,7 +1156,7 @@ int launch_dkv(const AttnJob& j, const AttnSplit& sp, hipStream_t st) {
 template <typename T, int DP>
 int pass_rows(const AttnJob& j, float* ws, bool backward, hipStream_t st) {
   const int64_t rows = (int64_t)j.s.batch * j.s.q_heads * j.s.q_rows;
-  AttnSplit sp = split_rows(j.s);
+  AttnSplit sp = split_rows(j.s, backward);
   sp.out[0] = ws;
   sp.stats = ws + sp.parts * rows * j.s.d_head;
   if constexpr (sizeof(T) == 2 || DP <= 64) {
@@ -1195,16 +1201,16 @@ static int64_t mask_words(const vf_attn_shape& s) { return ((int64_t)s.k_rows + 
 static int64_t mask_floats(const vf_attn_shape& s) { return round4(2 * s.batch * mask_words(s)); }
 int64_t attn_workspace_bytes(const vf_attn_shape& s, bool backward) {
   if (!s.batch || (!backward && !s.q_rows)) return 0;
-  const int64_t parts = part_rows_floats(s, split_rows(s));
+  const int64_t parts = part_rows_floats(s, split_rows(s, backward));
   if (!backward) return (mask_floats(s) + parts) * (int64_t)sizeof(float);
   const int64_t stats = 2 * round4((int64_t)s.batch * s.q_heads * s.q_rows);
   return (mask_floats(s) + stats + std::max(parts, part_keys_floats(s, split_keys(s)))) * (int64_t)sizeof(float);
 }
 
-static int make_bits(AttnJob& j, float* ws, hipStream_t st) {
+static int make_bits(AttnJob& j, bool backward, float* ws, hipStream_t st) {
   j.words = (int)mask_words(j.s);
   const int64_t n = (int64_t)j.s.batch * j.words;
-  const AttnSplit sp = split_rows(j.s);
+  const AttnSplit sp = split_rows(j.s, backward);
   const int tile = std::max(j.s.dtype == VF_BF16 ? Elem<bf16_t>::TR : Elem<float>::TR, 32 * sp.sw);
   if (!j.key_mask || !n || !j.s.q_rows || (int64_t)sp.per * tile <= kMaskWords * 64) return VF_OK;
   j.bits = reinterpret_cast<uint64_t*>(ws);
@@ -1216,7 +1222,7 @@ static int make_bits(AttnJob& j, float* ws, hipStream_t st) {
 int launch_attn(AttnJob j, void* workspace, hipStream_t st) {
   if (!j.s.batch || !j.s.q_rows) return VF_OK;
   float* ws = static_cast<float*>(workspace);
-  VF_TRY(make_bits(j, ws, st));
+  VF_TRY(make_bits(j, false, ws, st));
   ws += mask_floats(j.s);
   if (j.s.dtype == VF_BF16) return by_width(j.s.d_head, [&](auto dp) { return pass_rows<bf16_t, decltype(dp)::value>(j, ws, false, st); });
   return by_width(j.s.d_head, [&](auto dp) { return pass_rows<float, decltype(dp)::value>(j, ws, false, st); });
@@ -1225,7 +1231,7 @@ int launch_attn(AttnJob j, void* workspace, hipStream_t st) {
 int launch_attn_bwd(AttnJob j, void* workspace, hipStream_t st) {
   if (!j.s.batch || (!j.s.q_rows && !j.s.k_rows)) return VF_OK;
   float* ws = static_cast<float*>(workspace);
-  VF_TRY(make_bits(j, ws, st));
+  VF_TRY(make_bits(j, true, ws, st));
   const int64_t rows = round4((int64_t)j.s.batch * j.s.q_heads * j.s.q_rows);
   j.row_lse = ws + mask_floats(j.s);
   j.row_delta = j.row_lse + rows;
