@@ -102,7 +102,7 @@ __device__ __forceinline__ void step_of(f32x16& acc, u32x4 x, u32x4 y) {
     for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(u[e], v[e], acc, 0, 0, 0);
   }
 }
-template <typename T, int DP, bool TWO, int AHEAD = 4, int BESIDE = 0>
+template <typename T, int DP, bool TWO, int AHEAD = 4>
 __device__ __forceinline__ void dot_rows(f32x16& accA, const T* ta, int ra, const Held<T, DP>& a, f32x16& accB, const T* tb, int rb,
                                          const Held<T, DP>& b, int lane) {
   constexpr int S = Held<T, DP>::STEPS, LOOK = S < AHEAD ? S : AHEAD, PAIR = TWO ? 2 : 1, OPS = PAIR * (sizeof(T) == 2 ? 1 : 4);
@@ -127,17 +127,8 @@ __device__ __forceinline__ void dot_rows(f32x16& accA, const T* ta, int ra, cons
   for (int s = 0; s < S - LOOK; ++s) {
     __builtin_amdgcn_sched_group_barrier(0x8, OPS, 0);             // matrix instructions
     __builtin_amdgcn_sched_group_barrier(0x100, PAIR, 0);
-    if constexpr (BESIDE > 0) __builtin_amdgcn_sched_group_barrier(0x2, BESIDE * PAIR, 0);   // vector instructions
   }
-  if constexpr (BESIDE > 0) {
-#pragma unroll
-    for (int s = 0; s < LOOK; ++s) {
-      __builtin_amdgcn_sched_group_barrier(0x8, OPS, 0);
-      __builtin_amdgcn_sched_group_barrier(0x2, BESIDE * PAIR, 0);
-    }
-  } else {
-    __builtin_amdgcn_sched_group_barrier(0x8, OPS * LOOK, 0);
-  }
+  __builtin_amdgcn_sched_group_barrier(0x8, OPS * LOOK, 0);
 }
 
 // Transposing read: elements (row0 + 4 half + 0..3, col0 + l % 32) and the same eight rows further down.
@@ -207,7 +198,8 @@ __device__ __forceinline__ void clear(f32x16 (&a)[N]) {
 // side), so a tile under way costs no registers, and a ring of STAGES buffers keeps STAGES - 1 of them under way.  The order of
 // chunks in LDS is made on the memory side: a lane fetches the chunk that belongs at its place.  Rows that are padding or
 // invisible and chunks behind the head come from a block of zeros: nothing that lies there in memory reaches a product.
-// Loads of a wavefront complete in order, so "all but the newest n" (vmcnt) says when a tile is there.
+// Loads of a wavefront complete in order, so "all but the newest n" (vmcnt) says when a tile is there.  (M0 holds a load's LDS address;
+// nothing else in these kernels uses it.)
 __device__ __attribute__((aligned(16))) uint32_t g_zeros[4];
 __device__ uint32_t g_infinity = 0x7f800000u;
 
@@ -225,6 +217,13 @@ __device__ __forceinline__ void lds_load4(const void* src, uint32_t dst) {
 template <int N>
 __device__ __forceinline__ void wait_and_meet() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// ... for the next tile of a ring: all but the STAGES - 2 tiles behind it, of LOADS loads each, or, at the end of the stream, all
+template <int STAGES, int LOADS>
+__device__ __forceinline__ void meet_for_tile(bool more) {
+  if (STAGES == 2 || !more) wait_and_meet<0>();
+  else wait_and_meet<(STAGES - 2) * LOADS>();
 }
 
 template <typename T, int DP, int SW>
@@ -300,25 +299,31 @@ struct Source {
       off[i] = (near ? (uint32_t)ro.t * (uint32_t)row_b + (uint32_t)ro.g * (uint32_t)head_b : 0) + elem(i) * (uint32_t)sizeof(T);
     }
   }
-  // bit i: chunk i lies within the head
-  static __device__ __forceinline__ uint32_t head_bits(int dh) {
-    uint32_t m = 0;
+  // Which of this thread's chunks are wanted: those of rows whose bit is set, within the head.
+  static __device__ __forceinline__ void wanted(const uint64_t (&rows)[WORDS], int dh, bool (&on)[N]) {
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (elem(i) < dh) m |= 1u << i;
-    return m;
-  }
-  // Tile from row r0 on.  rows: bit r: row r of the tile is wanted; whole: all of them, and the head fills its chunks; tile: LDS
-  // address of the tile's buffer for this wavefront
-  __device__ __forceinline__ void issue(const AttnJob& j, int r0, const uint64_t (&rows)[WORDS], uint32_t head, bool whole, const char* zeros,
-                                        uint32_t tile) const {
-    const RowOf first = GROUPED ? row_of(j, r0) : RowOf{r0, 0};
-    const char* from = base + first.t * row_b;
-    if (near && whole) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) lds_load16(from, off[i], tile + i * (NT * 16));
-      return;
+    for (int i = 0; i < N; ++i) {
+      if constexpr (NT % CH == 0) {                         // (a load's rows lie within one word)
+        const uint64_t word = rows[i * (NT / CH) / 64] >> (threadIdx.x / CH);
+        on[i] = (uint32_t)(word >> (i * (NT / CH) % 64)) & 1;
+      } else {
+        const int r = row(i);
+        on[i] = (uint32_t)((WORDS > 1 && r >= 64 ? rows[WORDS - 1] : rows[0]) >> (r & 63)) & 1;
+      }
+      if (dh < DP) on[i] = on[i] && elem(i) < dh;
     }
+  }
+  // The tile's first row
+  __device__ __forceinline__ const char* start(const AttnJob& j, int r0) const { return base + (GROUPED ? row_of(j, r0) : RowOf{r0, 0}).t * row_b; }
+  // Tile from row r0 on, all of it.  tile: LDS address of the tile's buffer for this wavefront
+  __device__ __forceinline__ void issue(const AttnJob& j, int r0, uint32_t tile) const {
+    const char* from = start(j, r0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) lds_load16(from, off[i], tile + i * (NT * 16));
+  }
+  // ... the wanted chunks; zeros for the others
+  __device__ __forceinline__ void issue(const AttnJob& j, int r0, const bool (&on)[N], const char* zeros, uint32_t tile) const {
+    const char* from = start(j, r0);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const char* p = from + off[i];
@@ -326,22 +331,29 @@ struct Source {
         const RowOf ro = GROUPED ? row_of(j, r0 + row(i)) : RowOf{r0 + row(i), 0};
         p = base + ro.t * row_b + ro.g * head_b + off[i];
       }
-      uint64_t wanted;
-      if constexpr (NT % CH == 0) {                         // (a load's rows lie within one word)
-        wanted = rows[i * (NT / CH) / 64] >> (threadIdx.x / CH) >> (i * (NT / CH) % 64);
-      } else {
-        const int r = row(i);
-        wanted = (WORDS > 1 && r >= 64 ? rows[WORDS - 1] : rows[0]) >> (r & 63);
-      }
-      lds_load16((wanted & (head >> i) & 1) ? p : zeros, tile + i * (NT * 16));
+      lds_load16(on[i] ? p : zeros, tile + i * (NT * 16));
     }
   }
 };
+// A pair of tiles (rows r0 on of two tensors): rows as bits; whole: all of them, and the head fills its chunks.
+template <typename S>
+__device__ __forceinline__ void issue_pair(const AttnJob& j, const S& a, const S& b, int r0, const uint64_t (&rows)[S::WORDS], bool whole, int dh,
+                                           const char* zeros, uint32_t tile_a, uint32_t tile_b) {
+  if (whole && a.near && b.near) {
+    a.issue(j, r0, tile_a);
+    b.issue(j, r0, tile_b);
+    return;
+  }
+  bool on[S::N];
+  S::wanted(rows, dh, on);
+  a.issue(j, r0, on, zeros, tile_a);
+  b.issue(j, r0, on, zeros, tile_b);
+}
 
 __device__ __forceinline__ uint64_t first_bits(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; }
 // An address in scalar registers that is not taken again in the loops.
-__device__ __forceinline__ const char* zeros_address() {
-  const char* z = reinterpret_cast<const char*>(g_zeros);
+__device__ __forceinline__ const char* fixed_address(const void* p) {
+  const char* z = static_cast<const char*>(p);
   asm volatile("" : "+s"(z));
   return z;
 }
@@ -506,12 +518,11 @@ __global__ __launch_bounds__(NT, (fwd_waves<T, DP>())) void xattn_fwd_kernel(Att
 
   const Mask mask = take_mask(j, p, xattn_lds + R::LDS, kbeg, kend);
   const uint32_t lds0 = lds_address(lds) + __builtin_amdgcn_readfirstlane(wave) * 1024;
-  const char* const zeros = zeros_address();
-  const uint32_t in_head = Source<T, DP, SW, false>::head_bits(dh);
+  const char* const zeros = fixed_address(g_zeros);
   Source<T, DP, SW, false> ks, vs;
   ks.init(j, at<const T>(j.k, j.s.k, p.b, 0, p.hk), j.s.k);
   vs.init(j, at<const T>(j.v, j.s.v, p.b, 0, p.hk), j.s.v);
-  auto issue = [&](int k0, int buf) {                       // (behind the last tile: zeros, so that every tile counts alike)
+  auto issue = [&](int k0, int buf) {
     uint64_t vis[WORDS], all = ~0ull;
 #pragma unroll
     for (int i = 0; i < WORDS; ++i) {
@@ -519,19 +530,18 @@ __global__ __launch_bounds__(NT, (fwd_waves<T, DP>())) void xattn_fwd_kernel(Att
       all &= vis[i];
     }
     const bool whole = dh == DP && (all & ALL) == ALL;
-    ks.issue(j, k0, vis, in_head, whole, zeros, lds0 + buf * 2 * BYTES);
-    vs.issue(j, k0, vis, in_head, whole, zeros, lds0 + buf * 2 * BYTES + BYTES);
+    issue_pair(j, ks, vs, k0, vis, whole, dh, zeros, lds0 + buf * 2 * BYTES, lds0 + buf * 2 * BYTES + BYTES);
   };
-  if (kbeg < kend) {
 #pragma unroll
-    for (int i = 0; i < STAGES - 1; ++i) issue(kbeg + i * TR, i);
-  }
+  for (int i = 0; i < STAGES - 1; ++i)
+    if (kbeg + i * TR < kend) issue(kbeg + i * TR, i);
   q.arrive();
   auto step = [&](auto buf, int k0) {
     const T* kt = lds + buf * 2 * ELEMS;
     const T* vt = kt + ELEMS;
-    wait_and_meet<(STAGES - 2) * 2 * R::N>();     // this tile is there, and nobody reads the one before it
-    issue(k0 + (STAGES - 1) * TR, (buf + STAGES - 1) % STAGES);
+    const int ahead = k0 + (STAGES - 1) * TR;               // this tile is there, and nobody reads the one before it:
+    meet_for_tile<STAGES, 2 * R::N>(ahead < kend);
+    if (ahead < kend) issue(ahead, (buf + STAGES - 1) % STAGES);
     const uint64_t now = visible(j, p, mask, k0 + 32 * block);
     f32x16 s[KB];
     if constexpr (KB == 2) {
@@ -602,7 +612,6 @@ __global__ __launch_bounds__(NT, (fwd_waves<T, DP>())) void xattn_fwd_kernel(Att
     int buf = 0;
     for (int k0 = kbeg; k0 < kend; k0 += TR, buf = (buf + 1) % STAGES) step(buf, k0);
   }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // no load may find its LDS given away
   l = pair_sum(l);
   if constexpr (SW > 1) {
     // the wavefronts' maxima and sums, then their results weighed by them
@@ -688,12 +697,11 @@ __global__ __launch_bounds__(NT, (dq_waves<T, DP, SW, EXACT>())) void xattn_dq_k
 
   const Mask mask = take_mask(j, p, xattn_lds + R::LDS, kbeg, kend);
   const uint32_t lds0 = lds_address(lds) + __builtin_amdgcn_readfirstlane(wave) * 1024;
-  const char* const zeros = zeros_address();
-  const uint32_t in_head = Source<T, DP, SW, false>::head_bits(dh);
+  const char* const zeros = fixed_address(g_zeros);
   Source<T, DP, SW, false> ks, vs;
   ks.init(j, at<const T>(j.k, j.s.k, p.b, 0, p.hk), j.s.k);
   vs.init(j, at<const T>(j.v, j.s.v, p.b, 0, p.hk), j.s.v);
-  auto issue = [&](int k0, int buf) {                       // (behind the last tile: zeros, so that every tile counts alike)
+  auto issue = [&](int k0, int buf) {
     uint64_t vis[WORDS], all = ~0ull;
 #pragma unroll
     for (int i = 0; i < WORDS; ++i) {
@@ -701,13 +709,11 @@ __global__ __launch_bounds__(NT, (dq_waves<T, DP, SW, EXACT>())) void xattn_dq_k
       all &= vis[i];
     }
     const bool whole = dh == DP && (all & ALL) == ALL;
-    ks.issue(j, k0, vis, in_head, whole, zeros, lds0 + buf * 2 * BYTES);
-    vs.issue(j, k0, vis, in_head, whole, zeros, lds0 + buf * 2 * BYTES + BYTES);
+    issue_pair(j, ks, vs, k0, vis, whole, dh, zeros, lds0 + buf * 2 * BYTES, lds0 + buf * 2 * BYTES + BYTES);
   };
-  if (kbeg < kend) {
 #pragma unroll
-    for (int i = 0; i < STAGES - 1; ++i) issue(kbeg + i * TR, i);
-  }
+  for (int i = 0; i < STAGES - 1; ++i)
+    if (kbeg + i * TR < kend) issue(kbeg + i * TR, i);
   Held<T, DP> q, g;
   q.load(live ? at<const T>(j.q, j.s.q, p.b, ro.t, head) : nullptr, dh, half);
   g.load(live ? at<const T>(j.d_o, j.s.d_o, p.b, ro.t, head) : nullptr, dh, half);
@@ -733,8 +739,9 @@ __global__ __launch_bounds__(NT, (dq_waves<T, DP, SW, EXACT>())) void xattn_dq_k
   auto step = [&](auto buf, int k0) {
     const T* kt = lds + buf * 2 * ELEMS;
     const T* vt = kt + ELEMS;
-    wait_and_meet<(STAGES - 2) * 2 * R::N>();     // this tile is there, and nobody reads the one before it
-    issue(k0 + (STAGES - 1) * TR, (buf + STAGES - 1) % STAGES);
+    const int ahead = k0 + (STAGES - 1) * TR;               // this tile is there, and nobody reads the one before it:
+    meet_for_tile<STAGES, 2 * R::N>(ahead < kend);
+    if (ahead < kend) issue(ahead, (buf + STAGES - 1) % STAGES);
     const uint64_t now = visible(j, p, mask, k0 + 32 * block);
 #pragma unroll 1
     for (int kb = 0; kb < KB; ++kb) {
@@ -771,7 +778,6 @@ __global__ __launch_bounds__(NT, (dq_waves<T, DP, SW, EXACT>())) void xattn_dq_k
     int buf = 0;
     for (int k0 = kbeg; k0 < kend; k0 += TR, buf = (buf + 1) % STAGES) step(buf, k0);
   }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   rest = pair_sum(rest);
   if constexpr (SW > 1) {
     float* rows = reinterpret_cast<float*>(xattn_lds);
@@ -817,8 +823,10 @@ __global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void xattn_dkv_kernel(Att
   using R = Ring<T, DP, SW>;
   constexpr int TR = R::TR, QB = TR / 32 / SW, RW = 4 / SW, ELEMS = R::ELEMS, STAGES = R::STAGES, BYTES = R::BYTES;
   constexpr int WORDS = Source<T, DP, SW, false>::WORDS, STAT = 64 * WORDS;   // rows of statistics of a stage
-  constexpr bool BOTH = false;
-  constexpr int UNROLL = DP * sizeof(T) <= 128 ? 1 : 2, BESIDE = 6;
+  // blocks of 32 rows of a tile: bf16 heads of 64 take them one by one and leave out what lies behind the last row; wider ones keep
+  // both in one piece of code for the scheduler (16 problems of 8192 rows x 4096 keys x 128: 650 us, one by one 720)
+  constexpr bool ONE_BY_ONE = DP * sizeof(T) <= 128;
+  constexpr int UNROLL = ONE_BY_ONE ? 1 : 2;
   constexpr uint64_t ALL = TR >= 64 ? ~0ull : (1ull << TR) - 1;
   extern __shared__ __attribute__((aligned(16))) char xattn_lds[];
   T* lds = reinterpret_cast<T*>(xattn_lds);                 // [STAGES][q, dO][ELEMS], then [STAGES][lse, delta][STAT]
@@ -841,10 +849,9 @@ __global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void xattn_dkv_kernel(Att
 
   const int rows = p.q_len * j.group;                       // padding lies behind them
   const uint32_t lds0 = lds_address(lds) + __builtin_amdgcn_readfirstlane(wave) * 1024, stats0 = lds_address(stats);
-  const char* const zeros = zeros_address();
+  const char *const zeros = fixed_address(g_zeros), *const infinity = fixed_address(&g_infinity);
   const int beg = w.first * TR, stop = min(rows, beg + sp.per * TR);
-  const int end = key0 < p.keys ? stop : beg;  // (a tile without a visible key: nothing but zeros to write)
-  const uint32_t in_head = Source<T, DP, SW, false>::head_bits(dh);
+  const int end = key0 < p.keys ? stop : beg;               // (a tile without a visible key: nothing but zeros to write)
   Source<T, DP, SW, true> qs, gs;
   qs.init(j, at<const T>(j.q, j.s.q, p.b, 0, p.hk * j.group), j.s.q);
   gs.init(j, at<const T>(j.d_o, j.s.d_o, p.b, 0, p.hk * j.group), j.s.d_o);
@@ -856,8 +863,7 @@ __global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void xattn_dkv_kernel(Att
       all &= want[i];
     }
     const bool whole = dh == DP && (all & ALL) == ALL;
-    qs.issue(j, r0, want, in_head, whole, zeros, lds0 + buf * 2 * BYTES);
-    gs.issue(j, r0, want, in_head, whole, zeros, lds0 + buf * 2 * BYTES + BYTES);
+    issue_pair(j, qs, gs, r0, want, whole, dh, zeros, lds0 + buf * 2 * BYTES, lds0 + buf * 2 * BYTES + BYTES);
     // every wavefront loads the statistics of the tile's rows (the same values to the same place: all count alike)
 #pragma unroll
     for (int i = 0; i < WORDS; ++i) {
@@ -865,14 +871,13 @@ __global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void xattn_dkv_kernel(Att
       const bool in = row < stop;
       const int64_t at_row = (int64_t)w.id * p.rows + row;
       const uint32_t dst = stats0 + (buf * 2 * STAT + 64 * i) * 4;
-      lds_load4(in ? static_cast<const void*>(j.row_lse + at_row) : &g_infinity, dst);
+      lds_load4(in ? static_cast<const void*>(j.row_lse + at_row) : static_cast<const void*>(infinity), dst);
       lds_load4(in ? static_cast<const void*>(j.row_delta + at_row) : static_cast<const void*>(zeros), dst + STAT * 4);
     }
   };
-  if (beg < end) {
 #pragma unroll
-    for (int i = 0; i < STAGES - 1; ++i) issue(beg + i * TR, i);
-  }
+  for (int i = 0; i < STAGES - 1; ++i)
+    if (beg + i * TR < end) issue(beg + i * TR, i);
   k.load(seen ? at<const T>(j.k, j.s.k, p.b, key, p.hk) : nullptr, dh, half);
   v.load(seen ? at<const T>(j.v, j.s.v, p.b, key, p.hk) : nullptr, dh, half);
   k.arrive();
@@ -881,8 +886,9 @@ __global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void xattn_dkv_kernel(Att
     const T* qt = lds + buf * 2 * ELEMS;
     const T* gt = qt + ELEMS;
     const float* st = stats + buf * 2 * STAT;
-    wait_and_meet<(STAGES - 2) * (2 * R::N + 2 * WORDS)>();
-    issue(r0 + (STAGES - 1) * TR, (buf + STAGES - 1) % STAGES);
+    const int ahead = r0 + (STAGES - 1) * TR;
+    meet_for_tile<STAGES, 2 * R::N + 2 * WORDS>(ahead < end);
+    if (ahead < end) issue(ahead, (buf + STAGES - 1) % STAGES);
     // p, dz of 32 rows from their products
     auto weights = [&](f32x16& s, f32x16& dp, int row0) {
 #pragma unroll
@@ -897,41 +903,18 @@ __global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void xattn_dkv_kernel(Att
         }
       }
     };
-    if constexpr (BOTH) {
-      // Two blocks of 32 rows, one wavefront to a SIMD: the vector work of the first goes between the matrix instructions of the
-      // second, and that of the second between those that take the first one's results.
-      f32x16 s0, p0, s1, p1;
-      dot_rows<T, DP, true, 4>(s0, qt, 0, k, p0, gt, 0, v, lane);
-      dot_rows<T, DP, true, 4, BESIDE>(s1, qt, 32, k, p1, gt, 32, v, lane);
-      weights(s0, p0, 0);
-      dot_cols<T, DP>(dv, gt, 0, s0, lane);
-      dot_cols<T, DP>(dk, qt, 0, p0, lane);
-      __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-#pragma unroll
-      for (int i = 0; i < DP / 8; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-        __builtin_amdgcn_sched_group_barrier(0x2, BESIDE, 0);
-      }
-      weights(s1, p1, 32);
-      dot_cols<T, DP>(dv, gt, 32, s1, lane);
-      dot_cols<T, DP>(dk, qt, 32, p1, lane);
-      __builtin_amdgcn_sched_group_barrier(0x8, DP / 8, 0);
-    } else {
 #pragma unroll UNROLL
-      for (int qb = 0; qb < QB; ++qb) {
-        if (DP * sizeof(T) <= 128 && r0 + 32 * (block + qb) >= stop) break;
-        f32x16 s, dp;
-        dot_rows<T, DP, true, 4>(s, qt, 32 * (block + qb), k, dp, gt, 32 * (block + qb), v, lane);
-        weights(s, dp, 32 * (block + qb));
-        dot_cols<T, DP>(dv, gt, 32 * (block + qb), s, lane);
-        dot_cols<T, DP>(dk, qt, 32 * (block + qb), dp, lane);
-      }
+    for (int qb = 0; qb < QB; ++qb) {
+      if (ONE_BY_ONE && r0 + 32 * (block + qb) >= stop) break;
+      f32x16 s, dp;
+      dot_rows<T, DP, true, 4>(s, qt, 32 * (block + qb), k, dp, gt, 32 * (block + qb), v, lane);
+      weights(s, dp, 32 * (block + qb));
+      dot_cols<T, DP>(dv, gt, 32 * (block + qb), s, lane);
+      dot_cols<T, DP>(dk, qt, 32 * (block + qb), dp, lane);
     }
   };
   int buf = 0;
   for (int r0 = beg; r0 < end; r0 += TR, buf = (buf + 1) % STAGES) step(buf, r0);
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   // an invisible key's columns hold what its zeros gave: nothing of it is stored
   if (!seen) { clear(dk); clear(dv); }
   if constexpr (SW > 1) {
