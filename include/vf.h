@@ -346,8 +346,8 @@ int vf_gemm_noalloc(const void* A, int64_t lda, const void* B, int64_t ldb, floa
  * Conventions of these entry points, beside those at the top of this file
  *   - a tensor [rows, heads, d_head] or [batch, rows, heads, d_head] is given by a pointer and its
  *     strides in ELEMENTS; the elements of a head are contiguous.  Input strides may be any (0 repeats
- *     a row or head), output strides must keep the outputs apart; outputs overlap no input except
- *     where a call says so;
+ *     a row or head), output strides must keep the outputs apart; outputs overlap no input and
+ *     no other output except where a call says so;
  *   - device memory is on the current device; work is enqueued on `stream` (NULL = the default
  *     stream), nothing is allocated, nothing synchronises, and no state is kept between calls, so
  *     calls on different streams do not disturb each other as long as each has its own workspace.

@@ -239,6 +239,9 @@ def vf_gemm_noalloc(A, B, Cout, M: int, N: int, K: int, alpha: float = 1.0, accu
 # spends 2 to 4 us here and in ctypes beside the 3 to 4 us of a kernel launch.
 
 
+_MOST = 0x7fffffff            # (ctypes cuts larger integers off without a word)
+
+
 def _refuse(where: str, why: str):
     raise VfError(VF_EINVAL, where, why)
 
@@ -319,6 +322,8 @@ def vf_rope(x, y, plan: VfRopePlan, positions=None, first: int = 0, seq_len: int
     if len(shape) != 3 or y.shape != shape:
         _refuse(where, "x and y are [rows, heads, d_head]")
     rows, heads, dh = shape
+    if heads > _MOST or dh > _MOST:
+        _refuse(where, "a size is beyond 32 bits")
     rc = lib().vf_rope(code, x.data_ptr(), xs[0], xs[1], y.data_ptr(), ys[0], ys[1], rows, heads, dh,
                        None if positions is None else _side(where, positions, dev, (rows,), t.i32), first, seq_len, C.byref(plan),
                        bool(inverse), None if stream is None else stream.cuda_stream)
@@ -336,6 +341,8 @@ def vf_qk_norm_rope(x, y, q_heads: int, gamma_q=None, gamma_k=None, eps: float =
     if len(shape) != 3 or y.shape != shape:
         _refuse(where, "x and y are [rows, heads, d_head]")
     rows, heads, dh = shape
+    if heads > _MOST or dh > _MOST or not 0 <= q_heads <= heads:
+        _refuse(where, f"{q_heads} of {heads} heads of {dh}")
     rc = lib().vf_qk_norm_rope(code, x.data_ptr(), xs[0], xs[1], y.data_ptr(), ys[0], ys[1], rows, q_heads, heads - q_heads, dh,
                                _side(where, gamma_q, dev, (dh,), t.f32), _side(where, gamma_k, dev, (dh,), t.f32), eps,
                                _side(where, positions, dev, (rows,), t.i32), first, seq_len,
@@ -346,6 +353,8 @@ def vf_qk_norm_rope(x, y, q_heads: int, gamma_q=None, gamma_k=None, eps: float =
 
 def vf_qk_norm_rope_workspace(rows: int, q_heads: int, k_heads: int, d_head: int) -> int:
     """Bytes of workspace vf_qk_norm_rope_backward needs for gradients of the weights."""
+    if max(q_heads, k_heads, d_head) > _MOST:
+        _refuse("vf_qk_norm_rope_workspace", "a size is beyond 32 bits")
     n = int(lib().vf_qk_norm_rope_workspace(rows, q_heads, k_heads, d_head))
     if n < 0:
         _check(n, "vf_qk_norm_rope_workspace")
@@ -362,6 +371,8 @@ def vf_qk_norm_rope_backward(x, dy, dx, q_heads: int, gamma_q=None, gamma_k=None
     if len(shape) != 3 or dy.shape != shape or dx.shape != shape:
         _refuse(where, "x, dy and dx are [rows, heads, d_head]")
     rows, heads, dh = shape
+    if heads > _MOST or dh > _MOST or not 0 <= q_heads <= heads:
+        _refuse(where, f"{q_heads} of {heads} heads of {dh}")
     f32, one = t.f32, (dh,)
     ws, size = _space(where, workspace, dev)
     rc = lib().vf_qk_norm_rope_backward(
@@ -386,7 +397,7 @@ def _attn_sizes(where: str, code: int, q, k, v, scale):
     B, Tq, Hq, dh = shape
     if ks[0] != B or ks[3] != dh:
         _refuse(where, "q, k and v differ in batch or head size")
-    if max(B, Tq, ks[1], Hq, ks[2], dh) > 0x7fffffff:
+    if max(B, Tq, ks[1], Hq, ks[2], dh) > _MOST:
         _refuse(where, "a size is beyond 32 bits")
     return code, B, Tq, ks[1], Hq, ks[2], dh, dh ** -0.5 if scale is None else scale
 

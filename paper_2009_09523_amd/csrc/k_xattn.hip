@@ -613,13 +613,14 @@ __global__ __launch_bounds__(NT, (fwd_waves<T, DP>())) void xattn_fwd_kernel(Att
     for (int k0 = kbeg; k0 < kend; k0 += TR, buf = (buf + 1) % STAGES) step(buf, k0);
   }
   l = pair_sum(l);
+  if (!live) { clear(o); l = 0.f; }                         // (its zeros times an infinite key are NaN)
   if constexpr (SW > 1) {
     // the wavefronts' maxima and sums, then their results weighed by them
     float* rows = reinterpret_cast<float*>(xattn_lds);
     float* stat = rows + 128 * R::JOIN_PITCH;               // [128][maximum, sum], then [128] factors
     const int slot = wave * WR + (lane & 31);
     __syncthreads();                                        // nobody reads a tile any more
-    if (half == 0) *reinterpret_cast<float2*>(stat + 2 * slot) = make_float2(m, live ? l : 0.f);
+    if (half == 0) *reinterpret_cast<float2*>(stat + 2 * slot) = make_float2(m, l);
     __syncthreads();
     float top = -INFINITY, total = 0.f;
 #pragma unroll
@@ -633,7 +634,7 @@ __global__ __launch_bounds__(NT, (fwd_waves<T, DP>())) void xattn_fwd_kernel(Att
       const float2 x = *reinterpret_cast<const float2*>(stat + 2 * ((k * RW + wave % RW) * WR + (lane & 31)));
       if (x.y != 0.f) total = fmaf(x.y, __builtin_amdgcn_exp2f((x.x - top) * c), total);
     }
-    const float mine_w = live && l != 0.f ? __builtin_amdgcn_exp2f((m - top) * c) : 0.f;
+    const float mine_w = l != 0.f ? __builtin_amdgcn_exp2f((m - top) * c) : 0.f;
     const float factor = sp.parts > 1 ? 1.f : total != 0.f ? 1.f / total : 0.f;
     store_row<float, DP>(rows + slot * R::JOIN_PITCH, o, mine_w, DP, half);
     if (wave < RW && half == 0) {
@@ -650,12 +651,11 @@ __global__ __launch_bounds__(NT, (fwd_waves<T, DP>())) void xattn_fwd_kernel(Att
   if (!mine) return;
   if (sp.parts > 1) {                                       // a part: unnormalised, with its maximum and sum
     const int64_t row = part_row(j, p, w, r);
-    if (!live) l = 0.f;
     if (half == 0) *reinterpret_cast<float2*>(sp.stats + 2 * row) = make_float2(m, l);
     store_row<float, DP>(sp.out[0] + row * dh, o, l != 0.f ? 1.f : 0.f, dh, half);
     return;
   }
-  const bool any = live && l != 0.f;                        // (a NaN goes on)
+  const bool any = l != 0.f;                                // (a NaN goes on)
   store_row<T, DP>(at<T>(j.o, j.s.o, p.b, ro.t, head), o, any ? 1.f / l : 0.f, dh, half);
   if (j.lse && half == 0)
     j.lse[((int64_t)p.b * j.s.q_heads + head) * j.s.q_rows + ro.t] = any ? fmaf(m, j.s.scale, logf(l)) : -INFINITY;
@@ -779,6 +779,7 @@ __global__ __launch_bounds__(NT, (dq_waves<T, DP, SW, EXACT>())) void xattn_dq_k
     for (int k0 = kbeg; k0 < kend; k0 += TR, buf = (buf + 1) % STAGES) step(buf, k0);
   }
   rest = pair_sum(rest);
+  if (!live) { clear(dq); clear(pk); rest = 0.f; }          // (as in the forward kernel)
   if constexpr (SW > 1) {
     float* rows = reinterpret_cast<float*>(xattn_lds);
     float* stat = rows + 128 * R::JOIN_PITCH;               // [128] rests
@@ -826,7 +827,6 @@ __global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void xattn_dkv_kernel(Att
   // blocks of 32 rows of a tile: bf16 heads of 64 take them one by one and leave out what lies behind the last row; wider ones keep
   // both in one piece of code for the scheduler (16 problems of 8192 rows x 4096 keys x 128: 650 us, one by one 720)
   constexpr bool ONE_BY_ONE = DP * sizeof(T) <= 128;
-  constexpr int UNROLL = ONE_BY_ONE ? 1 : 2;
   constexpr uint64_t ALL = TR >= 64 ? ~0ull : (1ull << TR) - 1;
   extern __shared__ __attribute__((aligned(16))) char xattn_lds[];
   T* lds = reinterpret_cast<T*>(xattn_lds);                 // [STAGES][q, dO][ELEMS], then [STAGES][lse, delta][STAT]
@@ -846,6 +846,7 @@ __global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void xattn_dkv_kernel(Att
   f32x16 dk[DP / 32], dv[DP / 32];
   clear(dk);
   clear(dv);
+  bool lost = false;                                        // a row's lse is NaN: so are its p, which weight_of bounds all the same
 
   const int rows = p.q_len * j.group;                       // padding lies behind them
   const uint32_t lds0 = lds_address(lds) + __builtin_amdgcn_readfirstlane(wave) * 1024, stats0 = lds_address(stats);
@@ -903,6 +904,7 @@ __global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void xattn_dkv_kernel(Att
         }
       }
     };
+    constexpr int UNROLL = ONE_BY_ONE ? 1 : 2;
 #pragma unroll UNROLL
     for (int qb = 0; qb < QB; ++qb) {
       if (ONE_BY_ONE && r0 + 32 * (block + qb) >= stop) break;
@@ -912,10 +914,14 @@ __global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void xattn_dkv_kernel(Att
       dot_cols<T, DP>(dv, gt, 32 * (block + qb), s, lane);
       dot_cols<T, DP>(dk, qt, 32 * (block + qb), dp, lane);
     }
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) lost = lost || st[64 * i + lane] != st[64 * i + lane];
   };
   int buf = 0;
   for (int r0 = beg; r0 < end; r0 += TR, buf = (buf + 1) % STAGES) step(buf, r0);
   // an invisible key's columns hold what its zeros gave: nothing of it is stored
+  const bool any_lost = __any(lost);                        // (of the whole wavefront, whatever its own key)
+  const float dv_by = seen && any_lost ? NAN : 1.f;
   if (!seen) { clear(dk); clear(dv); }
   if constexpr (SW > 1) {
     float* rows = reinterpret_cast<float*>(xattn_lds);
@@ -928,7 +934,7 @@ __global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void xattn_dkv_kernel(Att
     join_waves<T, DP, SW>(rows, [&](int) { return f; }, key0, j.s.k_rows, dh, sp.parts > 1 ? sp.out[0] + part : nullptr,
                           [&](int r) { return at<T>(j.dk, j.s.dk, p.b, r, p.hk); });
     __syncthreads();
-    store_row<float, DP>(slot, dv, 1.f, DP, half);
+    store_row<float, DP>(slot, dv, dv_by, DP, half);
     __syncthreads();
     join_waves<T, DP, SW>(rows, [&](int) { return 1.f; }, key0, j.s.k_rows, dh, sp.parts > 1 ? sp.out[1] + part : nullptr,
                           [&](int r) { return at<T>(j.dv, j.s.dv, p.b, r, p.hk); });
@@ -938,11 +944,11 @@ __global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void xattn_dkv_kernel(Att
   if (sp.parts > 1) {
     const int64_t row = ((int64_t)w.part * j.s.batch * j.s.kv_heads + w.id) * j.s.k_rows + key;
     store_row<float, DP>(sp.out[0] + row * dh, dk, 1.f, dh, half);
-    store_row<float, DP>(sp.out[1] + row * dh, dv, 1.f, dh, half);
+    store_row<float, DP>(sp.out[1] + row * dh, dv, dv_by, dh, half);
     return;
   }
   store_row<T, DP>(at<T>(j.dk, j.s.dk, p.b, key, p.hk), dk, j.s.scale, dh, half);
-  store_row<T, DP>(at<T>(j.dv, j.s.dv, p.b, key, p.hk), dv, 1.f, dh, half);
+  store_row<T, DP>(at<T>(j.dv, j.s.dv, p.b, key, p.hk), dv, dv_by, dh, half);
 }
 
 // ---- joining the parts -----------------------------------------------------------------------------------

@@ -236,7 +236,7 @@ int vf_attention(const vf_attn_shape* shape, const void* q, const void* k, const
   const vf_attn_shape& s = j.s;
   VF_TRY(make_job(shape, q, k, v, q_len, k_len, key_mask, &j));
   if (s.batch > 0 && s.q_rows > 0 && (!o || !aligned16(o))) return VF_EINVAL;
-  if (!output_apart(s.o, s.batch, s.q_rows, s.q_heads, s.d_head)) return VF_EINVAL;
+  if (!output_apart(s.o, s.batch, s.q_rows, s.q_heads, s.d_head) || (o && (o == q || o == k || o == v))) return VF_EINVAL;
   VF_TRY(check_workspace(s, false, workspace, workspace_bytes));
   j.o = o; j.lse = lse;
   return launch_attn(j, workspace, static_cast<hipStream_t>(stream));
@@ -256,6 +256,10 @@ int vf_attention_backward(const vf_attn_shape* shape, const void* q, const void*
   if (!output_apart(s.dq, s.batch, s.q_rows, s.q_heads, s.d_head) || !output_apart(s.dk, s.batch, s.k_rows, s.kv_heads, s.d_head) ||
       !output_apart(s.dv, s.batch, s.k_rows, s.kv_heads, s.d_head))
     return VF_EINVAL;
+  const void* outs[3] = {dq, dk, dv};
+  for (int i = 0; i < 3; ++i)                               // (an output is read again, as an input, by other workgroups)
+    for (const void* p : {q, k, v, o, d_o, static_cast<const void*>(outs[(i + 1) % 3])})
+      if (outs[i] && outs[i] == p) return VF_EINVAL;
   VF_TRY(check_workspace(s, true, workspace, workspace_bytes));
   j.o = const_cast<void*>(o); j.lse = const_cast<float*>(lse);
   j.d_o = d_o; j.dq = dq; j.dk = dk; j.dv = dv;

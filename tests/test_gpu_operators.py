@@ -468,6 +468,34 @@ def test_nan_in_a_visible_place_is_not_hidden():
     assert got["o"][0, 1].isnan().all() and got["o"][0, 0].isfinite().all() and got["o"][0, 2].isfinite().all()
 
 
+# one workgroup of whole tiles, wavefronts that share a tile, the streamed side in parts; each pass in turn
+NAN_SHAPES = [(1, 3, 70, 1, 1, 64), (16, 260, 90, 8, 8, 64), (16, 260, 90, 8, 8, 128), (2, 4, 9000, 4, 2, 64), (2, 3000, 20, 2, 1, 128)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("B,Tq,Tk,Hq,Hk,dh", NAN_SHAPES)
+def test_nan_in_a_query_reaches_the_gradients_of_its_keys(B, Tq, Tk, Hq, Hk, dh, dtype):
+    q, k, v, do = _inputs(B, Tq, Tk, Hq, Hk, dh, dtype)
+    q[0, 1, 0, 3] = math.nan                                  # every p of the row is NaN
+    got = _attend(q, k, v, do, dtype)
+    assert got["dq"][0, 1, 0].isnan().all() and got["dk"][0, :, 0].isnan().all() and got["dv"][0, :, 0].isnan().all()
+    assert got["dq"][0, 0].isfinite().all() and got["dq"][0, 2].isfinite().all()
+    for name in ("dk", "dv"):
+        assert got[name][1:].isfinite().all() and got[name][:, :, 1:].isfinite().all(), name
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("B,Tq,Tk,Hq,Hk,dh", NAN_SHAPES)
+def test_padded_rows_are_zero_beside_keys_that_are_not_finite(B, Tq, Tk, Hq, Hk, dh, dtype):
+    q, k, v, do = _inputs(B, Tq, Tk, Hq, Hk, dh, dtype)
+    k[0, 2], v[0, 5] = math.inf, math.nan
+    got = _attend(q, k, v, do, dtype, q_len=[2] * B)
+    for name in ("o", "dq"):
+        assert (got[name][:, 2:] == 0).all() and got[name][0, :2].isnan().all(), name
+        assert got[name][1:].isfinite().all(), name
+    assert (got["lse"][:, :, 2:] == -math.inf).all()
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_attention_over_other_orders(dtype):
     """Heads before rows; heads inside wider rows; keys and values shared by the batch (stride 0)."""
@@ -600,6 +628,17 @@ def test_operators_on_another_stream_and_in_a_graph():
         for a, b in zip(replayed, outs):
             assert torch.equal(a, b), turn
     assert not torch.equal(eager[0], outs[0])
+
+
+def test_heads_that_are_not_there_are_refused():
+    import torch
+    import paper_2009_09523_amd as vf
+    x = torch.zeros(2, 3, 64, device="cuda")
+    y = torch.empty_like(x)
+    for heads in (-1, 4, 1 << 32):
+        for call in (lambda: vf.vf_qk_norm_rope(x, y, heads), lambda: vf.vf_qk_norm_rope_backward(x, x, y, heads)):
+            with pytest.raises(vf.VfError):
+                call()
 
 
 def test_two_calls_at_once_keep_apart():

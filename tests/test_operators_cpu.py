@@ -162,6 +162,22 @@ def test_attention_refused():
         assert _backward(_shape(**{n: l})) == EINVAL, n
 
 
+def test_attention_refuses_outputs_in_place():
+    s = _shape()
+    for n in ("q", "k", "v"):
+        assert _forward(s, **{"q": 3 * P, "k": 4 * P, "v": 5 * P, n: 2 * P}) == EINVAL, n
+    apart = dict(zip(("q", "k", "v", "o", "d_o", "dq", "dk", "dv"), range(P, 9 * P, P)))
+    for out in ("dq", "dk", "dv"):
+        for n in apart:
+            if n != out:
+                assert _backward(s, **(apart | {out: apart[n]})) == EINVAL, (out, n)
+
+
+def test_sizes_beyond_32_bits_are_refused():
+    with pytest.raises(vf.VfError):
+        vf.vf_qk_norm_rope_workspace(4, (1 << 32) + 1, 1, 64)
+
+
 def test_nothing_to_attend_is_a_no_op():
     assert _forward(_shape(batch=0), None, None, None, None, ws=None, bytes=0) == 0
     assert _forward(_shape(q_rows=0), None, P, P, None, ws=None, bytes=0) == 0
