@@ -415,7 +415,8 @@ __device__ __forceinline__ float other_half(float v, float* mine) {
 __device__ __forceinline__ float pair_max(float v) { float a; const float b = other_half(v, &a); return fmaxf(a, b); }
 __device__ __forceinline__ float pair_sum(float v) { float a; const float b = other_half(v, &a); return a + b; }
 
-// An accumulator over the head (elements down, held rows across), times `f`, to the lane's row.
+// An accumulator over the head (elements down, held rows across), times `f`, to the lane's row; zeros where f is 0, whatever the
+// accumulator holds.  (Cleared ahead of this instead, the loop before it keeps its accumulators elsewhere: twice the time.)
 template <typename T, int DP>
 __device__ __forceinline__ void store_row(T* row, const f32x16 (&acc)[DP / 32], float f, int dh, int half) {
 #pragma unroll
@@ -424,7 +425,10 @@ __device__ __forceinline__ void store_row(T* row, const f32x16 (&acc)[DP / 32], 
     for (int g = 0; g < 4; ++g) {
       const int e = 32 * db + 8 * g + 4 * half;
       if (e >= dh) continue;
-      const float a = acc[db][4 * g] * f, b = acc[db][4 * g + 1] * f, c = acc[db][4 * g + 2] * f, d = acc[db][4 * g + 3] * f;
+      float x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = f != 0.f ? acc[db][4 * g + i] * f : 0.f;
+      const float a = x[0], b = x[1], c = x[2], d = x[3];
       if constexpr (sizeof(T) == 2) {
         *reinterpret_cast<uint2*>(row + e) = make_uint2(f32x2_to_bf16x2(a, b), f32x2_to_bf16x2(c, d));
       } else {
@@ -441,8 +445,8 @@ __device__ __forceinline__ void remove(f32x16 (&a)[N], const f32x16 (&b)[N], flo
 #pragma unroll
     for (int r = 0; r < 16; ++r) a[i][r] = fmaf(-f, b[i][r], a[i][r]);
 }
-// Wavefronts to a SIMD that the kernels' registers are kept down to: two wherever that spills nothing (next to nothing at
-// fp32 of 64 with four wavefronts to a block), else one.
+// Wavefronts to a SIMD that the kernels' registers are kept down to: two wherever that spills nothing (next to nothing in
+// the dq kernel with four wavefronts to a block at fp32 of 64 and bf16 of 128), else one.
 template <typename T, int DP> constexpr int fwd_waves() { return DP * sizeof(T) <= 384 ? 2 : 1; }
 template <typename T, int DP, int SW, bool EXACT> constexpr int dq_waves() {
   return sizeof(T) == 4 ? (DP <= 64 ? 2 : 1) : !EXACT || DP <= 64 || (DP <= 96 && SW < 4) ? 2 : 1;
@@ -613,7 +617,7 @@ __global__ __launch_bounds__(NT, (fwd_waves<T, DP>())) void xattn_fwd_kernel(Att
     for (int k0 = kbeg; k0 < kend; k0 += TR, buf = (buf + 1) % STAGES) step(buf, k0);
   }
   l = pair_sum(l);
-  if (!live) { clear(o); l = 0.f; }                         // (its zeros times an infinite key are NaN)
+  if (!live) l = 0.f;                                       // (its zeros times an infinite key are NaN)
   if constexpr (SW > 1) {
     // the wavefronts' maxima and sums, then their results weighed by them
     float* rows = reinterpret_cast<float*>(xattn_lds);
@@ -779,7 +783,7 @@ __global__ __launch_bounds__(NT, (dq_waves<T, DP, SW, EXACT>())) void xattn_dq_k
     for (int k0 = kbeg; k0 < kend; k0 += TR, buf = (buf + 1) % STAGES) step(buf, k0);
   }
   rest = pair_sum(rest);
-  if (!live) { clear(dq); clear(pk); rest = 0.f; }          // (as in the forward kernel)
+  if (!live) rest = 0.f;                                    // (as in the forward kernel)
   if constexpr (SW > 1) {
     float* rows = reinterpret_cast<float*>(xattn_lds);
     float* stat = rows + 128 * R::JOIN_PITCH;               // [128] rests
@@ -791,7 +795,7 @@ __global__ __launch_bounds__(NT, (dq_waves<T, DP, SW, EXACT>())) void xattn_dq_k
 #pragma unroll
     for (int k = 0; k < SW; ++k) rest += stat[(k * RW + wave % RW) * WR + (lane & 31)];
     if constexpr (EXACT) remove(dq, pk, rest);
-    store_row<float, DP>(rows + slot * R::JOIN_PITCH, dq, 1.f, DP, half);
+    store_row<float, DP>(rows + slot * R::JOIN_PITCH, dq, live ? 1.f : 0.f, DP, half);
     __syncthreads();
     if (wave < RW && half == 0 && mine) {
       if (sp.parts > 1) *reinterpret_cast<float2*>(sp.stats + 2 * part_row(j, p, w, r)) = make_float2(rest, delta);
@@ -806,7 +810,7 @@ __global__ __launch_bounds__(NT, (dq_waves<T, DP, SW, EXACT>())) void xattn_dq_k
   if (sp.parts > 1) {
     const int64_t row = part_row(j, p, w, r);
     if (half == 0) *reinterpret_cast<float2*>(sp.stats + 2 * row) = make_float2(rest, delta);
-    store_row<float, DP>(sp.out[0] + row * dh, dq, 1.f, dh, half);
+    store_row<float, DP>(sp.out[0] + row * dh, dq, live ? 1.f : 0.f, dh, half);
     if (w.part == 0 && half == 0) j.row_lse[(int64_t)w.id * p.rows + r] = lse;
     return;
   }
@@ -815,7 +819,7 @@ __global__ __launch_bounds__(NT, (dq_waves<T, DP, SW, EXACT>())) void xattn_dq_k
     j.row_lse[(int64_t)w.id * p.rows + r] = lse;
     j.row_delta[(int64_t)w.id * p.rows + r] = delta + rest;
   }
-  store_row<T, DP>(at<T>(j.dq, j.s.dq, p.b, ro.t, head), dq, j.s.scale, dh, half);
+  store_row<T, DP>(at<T>(j.dq, j.s.dq, p.b, ro.t, head), dq, live ? j.s.scale : 0.f, dh, half);
 }
 
 // ---- backward: dk and dv ------------------------------------------------------------------------------
