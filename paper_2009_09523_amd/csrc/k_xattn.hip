@@ -848,7 +848,7 @@ __global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void xattn_dkv_kernel(Att
   constexpr int TR = R::TR, QB = TR / 32 / SW, RW = 4 / SW, ELEMS = R::ELEMS, STAGES = R::STAGES, BYTES = R::BYTES;
   constexpr int WORDS = Source<T, DP, SW, false>::WORDS, STAT = 64 * WORDS;   // rows of statistics of a stage
   // blocks of 32 rows of a tile: bf16 heads of 64 take them one by one and leave out what lies behind the last row; wider ones keep
-  // both in one piece of code for the scheduler (16 problems of 8192 rows x 4096 keys x 128: 650 us, one by one 720)
+  // both in one piece of code for the scheduler (16 problems of 8192 rows x 4096 keys x 128, with dq: 949 us, one by one 1015)
   constexpr bool ONE_BY_ONE = DP * sizeof(T) <= 128;
   constexpr uint64_t ALL = TR >= 64 ? ~0ull : (1ull << TR) - 1;
   extern __shared__ __attribute__((aligned(16))) char xattn_lds[];
