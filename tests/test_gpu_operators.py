@@ -397,6 +397,16 @@ def test_attention(B, Tq, Tk, Hq, Hk, dh, dtype):
     _check_attn(_attend(q, k, v, do, dtype), _attn_ref(q, k, v, do, None, None, None, dh ** -0.5, dtype))
 
 
+# heads of 32 elements and less have a width of their own in fp32: whole tiles, wavefronts that share a tile, parts
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("B,Tq,Tk,Hq,Hk,dh", [(16, 260, 90, 8, 8, 32), (12, 90, 400, 8, 4, 24), (1, 1, 20000, 1, 1, 32), (1, 3000, 20, 2, 1, 32),
+                                              (2, 33, 31, 3, 3, 16), (1, 40, 6000, 2, 2, 32), (2, 700, 129, 6, 2, 32)])
+def test_attention_of_short_heads(B, Tq, Tk, Hq, Hk, dh, dtype):
+    q, k, v, do = _inputs(B, Tq, Tk, Hq, Hk, dh, dtype)
+    k_len = None if B == 1 else [Tk - 7 * b for b in range(B)]
+    _check_attn(_attend(q, k, v, do, dtype, None, k_len), _attn_ref(q, k, v, do, None, k_len, None, dh ** -0.5, dtype))
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("B,Tq,Tk,Hq,Hk,dh,q_len,k_len", [
     (4, 70, 150, 2, 2, 64, [70, 1, 0, 33], [150, 64, 17, 0]),
