@@ -415,11 +415,11 @@ __device__ __forceinline__ float other_half(float v, float* mine) {
 __device__ __forceinline__ float pair_max(float v) { float a; const float b = other_half(v, &a); return fmaxf(a, b); }
 __device__ __forceinline__ float pair_sum(float v) { float a; const float b = other_half(v, &a); return a + b; }
 
-// An accumulator over the head (elements down, held rows across), times `f`, to the lane's row; zeros where f is 0, whatever the
+// An accumulator over the head (elements down, held rows across), times `f`, to the lane's row; zeros unless `any`, whatever the
 // accumulator holds.  (Cleared ahead of this instead, the loop before it keeps its accumulators elsewhere: twice the time.)
 template <typename T, int DP>
-__device__ __forceinline__ void store_row(T* row, const f32x16 (&acc)[DP / 32], float f, int dh, int half) {
-  auto value = [&](int db, int i) { return f != 0.f ? acc[db][i] * f : 0.f; };
+__device__ __forceinline__ void store_row(T* row, const f32x16 (&acc)[DP / 32], bool any, float f, int dh, int half) {
+  auto value = [&](int db, int i) { return any ? acc[db][i] * f : 0.f; };
   asm volatile("" : "+v"(half));                            // (or the loads' tests of the same elements are kept through the loop for this)
 #pragma unroll
   for (int db = 0; db < DP / 32; ++db) {
@@ -649,9 +649,9 @@ __global__ __launch_bounds__(NT, (fwd_waves<T, DP>())) void xattn_fwd_kernel(Att
       const float2 x = *reinterpret_cast<const float2*>(stat + 2 * ((k * RW + wave % RW) * WR + (lane & 31)));
       if (x.y != 0.f) total = fmaf(x.y, __builtin_amdgcn_exp2f((x.x - top) * c), total);
     }
-    const float mine_w = l != 0.f ? __builtin_amdgcn_exp2f((m - top) * c) : 0.f;
+    const float mine_w = __builtin_amdgcn_exp2f((m - top) * c);      // may be 0: what is not finite stays so all the same
     const float factor = sp.parts > 1 ? 1.f : total != 0.f ? 1.f / total : 0.f;
-    store_row<float, DP>(rows + slot * R::JOIN_PITCH, o, mine_w, DP, half);
+    store_row<float, DP>(rows + slot * R::JOIN_PITCH, o, l != 0.f, mine_w, DP, half);
     if (wave < RW && half == 0) {
       stat[256 + slot] = factor;
       if (mine) {
@@ -667,11 +667,11 @@ __global__ __launch_bounds__(NT, (fwd_waves<T, DP>())) void xattn_fwd_kernel(Att
   if (sp.parts > 1) {                                       // a part: unnormalised, with its maximum and sum
     const int64_t row = part_row(j, p, w, r);
     if (half == 0) *reinterpret_cast<float2*>(sp.stats + 2 * row) = make_float2(m, l);
-    store_row<float, DP>(sp.out[0] + row * dh, o, l != 0.f ? 1.f : 0.f, dh, half);
+    store_row<float, DP>(sp.out[0] + row * dh, o, l != 0.f, 1.f, dh, half);
     return;
   }
   const bool any = l != 0.f;                                // (a NaN goes on)
-  store_row<T, DP>(at<T>(j.o, j.s.o, p.b, ro.t, head), o, any ? 1.f / l : 0.f, dh, half);
+  store_row<T, DP>(at<T>(j.o, j.s.o, p.b, ro.t, head), o, any, 1.f / l, dh, half);
   if (j.lse && half == 0)
     j.lse[((int64_t)p.b * j.s.q_heads + head) * j.s.q_rows + ro.t] = any ? fmaf(m, j.s.scale, logf(l)) : -INFINITY;
 }
@@ -806,7 +806,7 @@ __global__ __launch_bounds__(NT, (dq_waves<T, DP, SW, EXACT>())) void xattn_dq_k
 #pragma unroll
     for (int k = 0; k < SW; ++k) rest += stat[(k * RW + wave % RW) * WR + (lane & 31)];
     if constexpr (EXACT) remove(dq, pk, rest);
-    store_row<float, DP>(rows + slot * R::JOIN_PITCH, dq, live ? 1.f : 0.f, DP, half);
+    store_row<float, DP>(rows + slot * R::JOIN_PITCH, dq, live, 1.f, DP, half);
     __syncthreads();
     if (wave < RW && half == 0 && mine) {
       if (sp.parts > 1) *reinterpret_cast<float2*>(sp.stats + 2 * part_row(j, p, w, r)) = make_float2(rest, delta);
@@ -821,7 +821,7 @@ __global__ __launch_bounds__(NT, (dq_waves<T, DP, SW, EXACT>())) void xattn_dq_k
   if (sp.parts > 1) {
     const int64_t row = part_row(j, p, w, r);
     if (half == 0) *reinterpret_cast<float2*>(sp.stats + 2 * row) = make_float2(rest, delta);
-    store_row<float, DP>(sp.out[0] + row * dh, dq, live ? 1.f : 0.f, dh, half);
+    store_row<float, DP>(sp.out[0] + row * dh, dq, live, 1.f, dh, half);
     if (w.part == 0 && half == 0) j.row_lse[(int64_t)w.id * p.rows + r] = lse;
     return;
   }
@@ -830,7 +830,7 @@ __global__ __launch_bounds__(NT, (dq_waves<T, DP, SW, EXACT>())) void xattn_dq_k
     j.row_lse[(int64_t)w.id * p.rows + r] = lse;
     j.row_delta[(int64_t)w.id * p.rows + r] = delta + rest;
   }
-  store_row<T, DP>(at<T>(j.dq, j.s.dq, p.b, ro.t, head), dq, live ? j.s.scale : 0.f, dh, half);
+  store_row<T, DP>(at<T>(j.dq, j.s.dq, p.b, ro.t, head), dq, live, j.s.scale, dh, half);
 }
 
 // Keeps accumulators in the accumulation registers at this point: left to itself the compiler copies three of the eight tiles out and
@@ -956,12 +956,12 @@ __global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void xattn_dkv_kernel(Att
     const float f = sp.parts > 1 ? 1.f : j.s.scale;
     float* slot = rows + (wave * WR + (lane & 31)) * R::JOIN_PITCH;
     __syncthreads();                                        // nobody reads a tile any more
-    store_row<float, DP>(slot, dk, 1.f, DP, half);
+    store_row<float, DP>(slot, dk, true, 1.f, DP, half);
     __syncthreads();
     join_waves<T, DP, SW>(rows, [&](int) { return f; }, key0, j.s.k_rows, dh, sp.parts > 1 ? sp.out[0] + part : nullptr,
                           [&](int r) { return at<T>(j.dk, j.s.dk, p.b, r, p.hk); });
     __syncthreads();
-    store_row<float, DP>(slot, dv, dv_by, DP, half);
+    store_row<float, DP>(slot, dv, true, dv_by, DP, half);
     __syncthreads();
     join_waves<T, DP, SW>(rows, [&](int) { return 1.f; }, key0, j.s.k_rows, dh, sp.parts > 1 ? sp.out[1] + part : nullptr,
                           [&](int r) { return at<T>(j.dv, j.s.dv, p.b, r, p.hk); });
@@ -970,12 +970,12 @@ __global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void xattn_dkv_kernel(Att
   if (!mine) return;
   if (sp.parts > 1) {
     const int64_t row = ((int64_t)w.part * j.s.batch * j.s.kv_heads + w.id) * j.s.k_rows + key;
-    store_row<float, DP>(sp.out[0] + row * dh, dk, 1.f, dh, half);
-    store_row<float, DP>(sp.out[1] + row * dh, dv, dv_by, dh, half);
+    store_row<float, DP>(sp.out[0] + row * dh, dk, true, 1.f, dh, half);
+    store_row<float, DP>(sp.out[1] + row * dh, dv, true, dv_by, dh, half);
     return;
   }
-  store_row<T, DP>(at<T>(j.dk, j.s.dk, p.b, key, p.hk), dk, j.s.scale, dh, half);
-  store_row<T, DP>(at<T>(j.dv, j.s.dv, p.b, key, p.hk), dv, dv_by, dh, half);
+  store_row<T, DP>(at<T>(j.dk, j.s.dk, p.b, key, p.hk), dk, true, j.s.scale, dh, half);
+  store_row<T, DP>(at<T>(j.dv, j.s.dv, p.b, key, p.hk), dv, true, dv_by, dh, half);
 }
 
 // ---- joining the parts -----------------------------------------------------------------------------------

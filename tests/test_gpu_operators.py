@@ -691,3 +691,28 @@ def test_offsets_beyond_32_bits():
     vf.vf_rope(kv[0], y, _plan(vf, dh, "half"), first=3)
     want, mag = _turn(torch.cat([k, v], 2)[0], torch.arange(Tk) + 3, dh, "half", _freqs(dh), 1.0)
     _close(y, want, mag * TURN + 2.0 ** -8 * want.abs(), "rope")
+
+
+# wavefronts that share a tile's keys (four, two), one wavefront to a row, the keys in parts
+FAR_SHAPES = [(1, 5, 200, 1, 1, 64), (32, 33, 257, 8, 8, 128), (16, 260, 90, 8, 8, 64), (2, 4, 9000, 4, 2, 64)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("B,Tq,Tk,Hq,Hk,dh", FAR_SHAPES)
+def test_values_that_are_not_finite_show_however_small_their_weight(B, Tq, Tk, Hq, Hk, dh, dtype):
+    """A visible key whose weight underflows to 0 beside another's: 0 times NaN or infinity is NaN, wherever the two keys lie."""
+    import torch
+    q, k, v, do = _inputs(B, Tq, Tk, Hq, Hk, dh, dtype)
+    q[0], G = 1.0, Hq // Hk
+    k[0] *= 0.01
+    for top in (3, Tk - 2):
+        kk = k.clone()
+        kk[0, top, 0] = 256.0 / dh ** 0.5                     # a score of 256 beside ones below 1: weights of exp(-255), below the range of fp32
+        for bad, value in ((1, math.nan), (33, math.inf), (66, -math.inf), (Tk - 1, math.nan)):
+            vv = v.clone()
+            vv[0, bad, 0, 5] = value
+            got = _attend(q, kk, vv, do, dtype)["o"]
+            where = (top, bad)
+            assert got[0, :, :G, 5].isnan().all(), where
+            got[0, :, :G, 5] = 0
+            assert got.isfinite().all(), where
