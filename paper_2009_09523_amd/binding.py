@@ -239,11 +239,17 @@ def vf_gemm_noalloc(A, B, Cout, M: int, N: int, K: int, alpha: float = 1.0, accu
 # spends 2 to 4 us here and in ctypes beside the 3 to 4 us of a kernel launch.
 
 
-_MOST = 0x7fffffff            # (ctypes cuts larger integers off without a word)
+_MOST, _MOST64 = 0x7fffffff, 0x7fffffffffffffff      # (ctypes cuts larger integers off without a word)
 
 
 def _refuse(where: str, why: str):
     raise VfError(VF_EINVAL, where, why)
+
+
+def _fit(where: str, most: int, *numbers: int):
+    for n in numbers:
+        if not -most <= n <= most:
+            _refuse(where, f"{n} is beyond {most.bit_length() + 1} bits")
 
 
 class _Torch:
@@ -307,9 +313,12 @@ def _space(where: str, t, dev: int):
 def vf_rope_make(layout: int, rot_dim: int, base: float = 10000.0, scaling: int = VF_ROPE_PLAIN, factor: float = 1.0,
                  trained_len: int = 0, beta_fast: float = 32.0, beta_slow: float = 1.0, scale: float = 1.0) -> VfRopePlan:
     """The plan of a position rotation (host only, plain data): kept and given to every call."""
-    plan = VfRopePlan()
-    _check(lib().vf_rope_make(int(layout), int(rot_dim), float(base), int(scaling), float(factor), int(trained_len),
-                              float(beta_fast), float(beta_slow), float(scale), C.byref(plan)), "vf_rope_make")
+    where, plan = "vf_rope_make", VfRopePlan()
+    layout, rot_dim, scaling, trained_len = int(layout), int(rot_dim), int(scaling), int(trained_len)
+    _fit(where, _MOST, layout, rot_dim, scaling)
+    _fit(where, _MOST64, trained_len)
+    _check(lib().vf_rope_make(layout, rot_dim, float(base), scaling, float(factor), trained_len, float(beta_fast), float(beta_slow),
+                              float(scale), C.byref(plan)), where)
     return plan
 
 
@@ -324,6 +333,7 @@ def vf_rope(x, y, plan: VfRopePlan, positions=None, first: int = 0, seq_len: int
     rows, heads, dh = shape
     if heads > _MOST or dh > _MOST:
         _refuse(where, "a size is beyond 32 bits")
+    _fit(where, _MOST64, first, seq_len)
     rc = lib().vf_rope(code, x.data_ptr(), xs[0], xs[1], y.data_ptr(), ys[0], ys[1], rows, heads, dh,
                        None if positions is None else _side(where, positions, dev, (rows,), t.i32), first, seq_len, C.byref(plan),
                        bool(inverse), None if stream is None else stream.cuda_stream)
@@ -343,6 +353,7 @@ def vf_qk_norm_rope(x, y, q_heads: int, gamma_q=None, gamma_k=None, eps: float =
     rows, heads, dh = shape
     if heads > _MOST or dh > _MOST or not 0 <= q_heads <= heads:
         _refuse(where, f"{q_heads} of {heads} heads of {dh}")
+    _fit(where, _MOST64, first, seq_len)
     rc = lib().vf_qk_norm_rope(code, x.data_ptr(), xs[0], xs[1], y.data_ptr(), ys[0], ys[1], rows, q_heads, heads - q_heads, dh,
                                _side(where, gamma_q, dev, (dh,), t.f32), _side(where, gamma_k, dev, (dh,), t.f32), eps,
                                _side(where, positions, dev, (rows,), t.i32), first, seq_len,
@@ -353,11 +364,12 @@ def vf_qk_norm_rope(x, y, q_heads: int, gamma_q=None, gamma_k=None, eps: float =
 
 def vf_qk_norm_rope_workspace(rows: int, q_heads: int, k_heads: int, d_head: int) -> int:
     """Bytes of workspace vf_qk_norm_rope_backward needs for gradients of the weights."""
-    if max(q_heads, k_heads, d_head) > _MOST:
-        _refuse("vf_qk_norm_rope_workspace", "a size is beyond 32 bits")
+    where = "vf_qk_norm_rope_workspace"
+    _fit(where, _MOST64, rows)
+    _fit(where, _MOST, q_heads, k_heads, d_head)
     n = int(lib().vf_qk_norm_rope_workspace(rows, q_heads, k_heads, d_head))
     if n < 0:
-        _check(n, "vf_qk_norm_rope_workspace")
+        _check(n, where)
     return n
 
 
@@ -373,6 +385,7 @@ def vf_qk_norm_rope_backward(x, dy, dx, q_heads: int, gamma_q=None, gamma_k=None
     rows, heads, dh = shape
     if heads > _MOST or dh > _MOST or not 0 <= q_heads <= heads:
         _refuse(where, f"{q_heads} of {heads} heads of {dh}")
+    _fit(where, _MOST64, first, seq_len)
     f32, one = t.f32, (dh,)
     ws, size = _space(where, workspace, dev)
     rc = lib().vf_qk_norm_rope_backward(

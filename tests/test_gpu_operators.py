@@ -716,3 +716,16 @@ def test_values_that_are_not_finite_show_however_small_their_weight(B, Tq, Tk, H
             assert got[0, :, :G, 5].isnan().all(), where
             got[0, :, :G, 5] = 0
             assert got.isfinite().all(), where
+
+
+@pytest.mark.parametrize("kw", [dict(first=1 << 64), dict(first=-(1 << 64)), dict(seq_len=(1 << 64) + 2), dict(seq_len=2 - (1 << 64))])
+def test_positions_beyond_64_bits_are_refused(kw):
+    """Cut to 64 bits they would be 0 and 2."""
+    import torch
+    import paper_2009_09523_amd as vf
+    x = torch.zeros(2, 3, 64, device="cuda")
+    plan = _plan(vf, 64, "half")
+    for call in (lambda: vf.vf_rope(x, x, plan, **kw), lambda: vf.vf_qk_norm_rope(x, x, 1, plan=plan, **kw),
+                 lambda: vf.vf_qk_norm_rope_backward(x, x, x, 1, plan=plan, **kw)):
+        with pytest.raises(vf.VfError):
+            call()

@@ -207,3 +207,21 @@ def test_binding_refuses_tensors_that_are_not_on_the_device():
         with pytest.raises(vf.VfError) as e:
             call()
         assert e.value.code == EINVAL
+
+
+@pytest.mark.parametrize("sizes", [((1 << 64) + 4, 1, 1, 64), (-(1 << 64) + 4, 1, 1, 64), (4, 1 - (1 << 32), 1, 64), (4, 1, 1 - (1 << 32), 64),
+                                   (4, 1, 1, 64 - (1 << 32)), (4, 1, 1, 64 + (1 << 32))])
+def test_workspaces_of_sizes_that_an_argument_does_not_hold_are_refused(sizes):
+    """Each of them is (4, 1, 1, 64) once cut to its argument's width."""
+    with pytest.raises(vf.VfError) as e:
+        vf.vf_qk_norm_rope_workspace(*sizes)
+    assert e.value.code == EINVAL
+
+
+@pytest.mark.parametrize("kw", [dict(layout=1 << 32), dict(rot=64 + (1 << 32)), dict(rot=64 - (1 << 32)), dict(scaling=1 << 32),
+                                dict(scaling=2, factor=2.0, trained_len=(1 << 64) + 9)])
+def test_plans_of_numbers_that_an_argument_does_not_hold_are_refused(kw):
+    a = dict(layout=0, rot=64) | kw
+    with pytest.raises(vf.VfError) as e:
+        vf.vf_rope_make(a.pop("layout"), a.pop("rot"), **a)
+    assert e.value.code == EINVAL
