@@ -380,7 +380,8 @@ typedef struct vf_rope_plan {
 } vf_rope_plan;
 
 /* Fills a plan; host only.  base > 1; LINEAR: factor > 0; PARTS: factor > 0, trained_len > 0 and
- * beta_fast > beta_slow (ignored otherwise); scale: factor of cosine and sine (1 normally). */
+ * beta_fast > beta_slow (ignored otherwise); scale: factor of cosine and sine (1 normally), within
+ * fp32; the frequencies have to come out finite. */
 int vf_rope_make(int32_t layout, int32_t rot_dim, double base, int32_t scaling, double factor,
                  int64_t trained_len, double beta_fast, double beta_slow, double scale,
                  vf_rope_plan* out);

@@ -1,6 +1,7 @@
 // C ABI of the operators between an attention block's projections: argument checks and the
 // rotation's frequencies; the kernels are in k_rope.hip and k_xattn.hip.
 #include <algorithm>
+#include <cfloat>
 #include <climits>
 #include <cmath>
 
@@ -126,15 +127,15 @@ extern "C" {
 int vf_rope_make(int32_t layout, int32_t rot_dim, double base, int32_t scaling, double factor, int64_t trained_len,
                  double beta_fast, double beta_slow, double scale, vf_rope_plan* out) {
   if (!out || (layout != VF_ROPE_HALF && layout != VF_ROPE_INTERLEAVED)) return VF_EINVAL;
-  if (rot_dim < 2 || rot_dim % 2 || rot_dim > 2 * VF_ROPE_MAX_PAIRS || !(base > 1.0) || !std::isfinite(base) || !std::isfinite(scale))
+  if (rot_dim < 2 || rot_dim % 2 || rot_dim > 2 * VF_ROPE_MAX_PAIRS || !(base > 1.0) || !std::isfinite(base) || !(std::fabs(scale) <= FLT_MAX))
     return VF_EINVAL;
   if (scaling != VF_ROPE_PLAIN && scaling != VF_ROPE_LINEAR && scaling != VF_ROPE_PARTS) return VF_EINVAL;
   if (scaling != VF_ROPE_PLAIN && (!(factor > 0.0) || !std::isfinite(factor))) return VF_EINVAL;
   if (scaling == VF_ROPE_PARTS && (trained_len < 1 || !(beta_fast > beta_slow) || !std::isfinite(beta_fast) || !std::isfinite(beta_slow)))
     return VF_EINVAL;
   const double two_pi = 6.283185307179586476925286766559;
-  *out = vf_rope_plan{};
-  out->layout = layout; out->rot_dim = rot_dim; out->scale = (float)scale;
+  vf_rope_plan plan{};
+  plan.layout = layout; plan.rot_dim = rot_dim; plan.scale = (float)scale;
   for (int j = 0; j < rot_dim / 2; ++j) {
     const double f = std::pow(base, -2.0 * j / rot_dim);
     double g = f;
@@ -143,8 +144,10 @@ int vf_rope_make(int32_t layout, int32_t rot_dim, double base, int32_t scaling, 
       const double keep = std::min(1.0, std::max(0.0, ((double)trained_len * f / two_pi - beta_slow) / (beta_fast - beta_slow)));
       g = keep * f + (1.0 - keep) * f / factor;
     }
-    out->turns[j] = g / two_pi;
+    plan.turns[j] = g / two_pi;
+    if (!std::isfinite(plan.turns[j])) return VF_EINVAL;     // (a factor so small that the quotient overflows)
   }
+  *out = plan;
   return VF_OK;
 }
 

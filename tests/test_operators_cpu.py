@@ -225,3 +225,11 @@ def test_plans_of_numbers_that_an_argument_does_not_hold_are_refused(kw):
     with pytest.raises(vf.VfError) as e:
         vf.vf_rope_make(a.pop("layout"), a.pop("rot"), **a)
     assert e.value.code == EINVAL
+
+
+@pytest.mark.parametrize("kw", [dict(scale=1e300), dict(scale=-1e39), dict(scale=math.inf), dict(scaling=1, factor=1e-320),
+                                dict(scaling=2, factor=1e-320, trained_len=4096)])
+def test_plans_that_come_out_infinite_are_refused(kw):
+    with pytest.raises(vf.VfError) as e:
+        vf.vf_rope_make(0, 64, **kw)
+    assert e.value.code == EINVAL
