@@ -172,7 +172,7 @@ int vf_qk_norm_rope(int32_t dtype, const void* x, int64_t x_row, int64_t x_head,
                     int64_t rows, int32_t q_heads, int32_t k_heads, int32_t d_head, const float* gamma_q, const float* gamma_k,
                     float eps, const int32_t* positions, int64_t first, int64_t seq_len, const vf_rope_plan* plan, void* stream) {
   bool empty;
-  if (q_heads < 0 || k_heads < 0 || !(eps >= 0.f)) return VF_EINVAL;
+  if (q_heads < 0 || k_heads < 0 || !(eps >= 0.f && eps <= FLT_MAX)) return VF_EINVAL;
   const int64_t heads = (int64_t)q_heads + k_heads;
   VF_TRY(check_heads(dtype, x, y, y_row, y_head, rows, heads, d_head, seq_len, plan, &empty));
   if (empty) return VF_OK;
@@ -200,7 +200,7 @@ int vf_qk_norm_rope_backward(int32_t dtype, const void* x, int64_t x_row, int64_
                              float* dgamma_q, float* dgamma_k, float alpha, int32_t accumulate, void* workspace,
                              int64_t workspace_bytes, void* stream) {
   bool empty;
-  if (q_heads < 0 || k_heads < 0 || !(eps >= 0.f)) return VF_EINVAL;
+  if (q_heads < 0 || k_heads < 0 || !(eps >= 0.f && eps <= FLT_MAX)) return VF_EINVAL;
   const int64_t heads = (int64_t)q_heads + k_heads;
   VF_TRY(check_heads(dtype, x, dx, dx_row, dx_head, rows, heads, d_head, seq_len, plan, &empty));
   if (!empty) {

@@ -233,3 +233,9 @@ def test_plans_that_come_out_infinite_are_refused(kw):
     with pytest.raises(vf.VfError) as e:
         vf.vf_rope_make(0, 64, **kw)
     assert e.value.code == EINVAL
+
+
+@pytest.mark.parametrize("backward", [False, True])
+def test_an_infinite_eps_is_refused(backward):
+    """(Also what a number beyond fp32 becomes in the call: every head would come out as zeros.)"""
+    assert _norm(backward, eps=math.inf) == EINVAL and _norm(backward, eps=1e39) == EINVAL
