@@ -388,10 +388,12 @@ int vf_rope_make(int32_t layout, int32_t rot_dim, double base, int32_t scaling, 
 
 /* Turns heads by their rows' positions.  x, y: [rows, heads, d_head], dtype VF_F32 or VF_BF16; pair
  * (a, b) of a row at position p becomes  s (a cos t - b sin t), s (b cos t + a sin t)  with the angle
- * t = 2 pi p turns[j] (reduced in float64: exact for far positions) and the plan's scale s;
+ * t = 2 pi p turns[j] (taken and reduced to a turn in float64: off by about 2^-52 t, below an fp32 rounding
+ * for positions of up to some 2^27) and the plan's scale s;
  * elements from rot_dim on are copied.  inverse != 0 turns by -t: with the same scale that is the
  * operator's backward pass (dx from dy).  positions: device int32 [rows], or NULL for
- * first + (seq_len > 0 ? row % seq_len : row).  d_head: rot_dim .. 512, heads: up to 8192.  y may be x (same strides). */
+ * first + (seq_len > 0 ? row % seq_len : row), first from -2^52 to 2^52.  d_head: rot_dim .. 512, heads: up to 8192, rows: up to
+ * 2^31 - 1 (here and in the two calls below; their heads are q_heads + k_heads).  y may be x (same strides). */
 int vf_rope(int32_t dtype, const void* x, int64_t x_row, int64_t x_head, void* y, int64_t y_row,
             int64_t y_head, int64_t rows, int32_t heads, int32_t d_head, const int32_t* positions,
             int64_t first, int64_t seq_len, const vf_rope_plan* plan, int32_t inverse, void* stream);

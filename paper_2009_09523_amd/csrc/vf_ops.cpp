@@ -12,6 +12,7 @@ using namespace vf;
 namespace {
 
 constexpr int64_t kMaxRows = INT32_MAX;
+constexpr int64_t kMaxFirst = int64_t(1) << 52;            // positions are taken to float64
 constexpr int kMaxHeads = 8192, kMaxHead = 512;            // (heads: an item's row is found by a multiplication that is exact up to there)
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
@@ -58,9 +59,10 @@ size_t size_of(int32_t dtype) { return dtype == VF_BF16 ? 2 : dtype == VF_F32 ? 
 
 // What the calls over [rows, heads, d_head] have in common.  0 rows or heads: *empty.
 int check_heads(int32_t dtype, const void* x, const void* y, int64_t y_row, int64_t y_head, int64_t rows, int64_t heads,
-                int32_t d_head, int64_t seq_len, const vf_rope_plan* plan, bool* empty) {
+                int32_t d_head, int64_t first, int64_t seq_len, const vf_rope_plan* plan, bool* empty) {
   const size_t esz = size_of(dtype);
-  if (!esz || rows < 0 || rows > kMaxRows || heads < 0 || heads > kMaxHeads || d_head < 1 || d_head > kMaxHead || seq_len < 0)
+  if (!esz || rows < 0 || rows > kMaxRows || heads < 0 || heads > kMaxHeads || d_head < 1 || d_head > kMaxHead || seq_len < 0 ||
+      first < -kMaxFirst || first > kMaxFirst)
     return VF_EINVAL;
   if (!plan_ok(plan, d_head)) return VF_EINVAL;
   *empty = rows == 0 || heads == 0;
@@ -156,7 +158,7 @@ int vf_rope(int32_t dtype, const void* x, int64_t x_row, int64_t x_head, void* y
             int32_t inverse, void* stream) {
   bool empty;
   if (!plan) return VF_EINVAL;
-  VF_TRY(check_heads(dtype, x, y, y_row, y_head, rows, heads, d_head, seq_len, plan, &empty));
+  VF_TRY(check_heads(dtype, x, y, y_row, y_head, rows, heads, d_head, first, seq_len, plan, &empty));
   if (empty) return VF_OK;
   if (!alias_ok(x, x_row, x_head, y, y_row, y_head, rows, heads)) return VF_EINVAL;
   RopeJob j{};
@@ -174,7 +176,7 @@ int vf_qk_norm_rope(int32_t dtype, const void* x, int64_t x_row, int64_t x_head,
   bool empty;
   if (q_heads < 0 || k_heads < 0 || !(eps >= 0.f && eps <= FLT_MAX)) return VF_EINVAL;
   const int64_t heads = (int64_t)q_heads + k_heads;
-  VF_TRY(check_heads(dtype, x, y, y_row, y_head, rows, heads, d_head, seq_len, plan, &empty));
+  VF_TRY(check_heads(dtype, x, y, y_row, y_head, rows, heads, d_head, first, seq_len, plan, &empty));
   if (empty) return VF_OK;
   if (!alias_ok(x, x_row, x_head, y, y_row, y_head, rows, heads)) return VF_EINVAL;
   RopeJob j{};
@@ -202,7 +204,7 @@ int vf_qk_norm_rope_backward(int32_t dtype, const void* x, int64_t x_row, int64_
   bool empty;
   if (q_heads < 0 || k_heads < 0 || !(eps >= 0.f && eps <= FLT_MAX)) return VF_EINVAL;
   const int64_t heads = (int64_t)q_heads + k_heads;
-  VF_TRY(check_heads(dtype, x, dx, dx_row, dx_head, rows, heads, d_head, seq_len, plan, &empty));
+  VF_TRY(check_heads(dtype, x, dx, dx_row, dx_head, rows, heads, d_head, first, seq_len, plan, &empty));
   if (!empty) {
     if (!dy || reinterpret_cast<uintptr_t>(dy) % size_of(dtype)) return VF_EINVAL;
     if (!alias_ok(x, x_row, x_head, dx, dx_row, dx_head, rows, heads) || !alias_ok(dy, dy_row, dy_head, dx, dx_row, dx_head, rows, heads))

@@ -239,3 +239,10 @@ def test_plans_that_come_out_infinite_are_refused(kw):
 def test_an_infinite_eps_is_refused(backward):
     """(Also what a number beyond fp32 becomes in the call: every head would come out as zeros.)"""
     assert _norm(backward, eps=math.inf) == EINVAL and _norm(backward, eps=1e39) == EINVAL
+
+
+@pytest.mark.parametrize("first", [(1 << 52) + 1, -(1 << 52) - 1, (1 << 63) - 1])
+def test_positions_that_float64_does_not_hold_are_refused(first):
+    for call in (_rope, _norm, lambda **kw: _norm(True, **kw)):
+        assert call(first=first) == EINVAL
+    assert _rope(first=1 << 52, rows=0) == 0 and _norm(first=-(1 << 52), rows=0) == 0
