@@ -400,6 +400,7 @@ def vf_qk_norm_rope_backward(x, dy, dx, q_heads: int, gamma_q=None, gamma_k=None
 
 _ATTN_SHAPE = struct.Struct("=7if24q")       # vf_attn_shape, field for field
 _ATTN_NONE = (0,) * 12
+_F32_MAX = 3.4028234663852886e38
 
 
 def _attn_sizes(where: str, code: int, q, k, v, scale):
@@ -412,7 +413,11 @@ def _attn_sizes(where: str, code: int, q, k, v, scale):
         _refuse(where, "q, k and v differ in batch or head size")
     if max(B, Tq, ks[1], Hq, ks[2], dh) > _MOST:
         _refuse(where, "a size is beyond 32 bits")
-    return code, B, Tq, ks[1], Hq, ks[2], dh, dh ** -0.5 if scale is None else scale
+    if scale is None:
+        scale = dh ** -0.5 if dh else 0.0                    # (heads of nothing: refused by the call)
+    elif not 0.0 < scale <= _F32_MAX:
+        _refuse(where, f"scale {scale}")
+    return code, B, Tq, ks[1], Hq, ks[2], dh, scale
 
 
 def _attn_masks(where: str, t: _Torch, dev: int, B: int, Tk: int, q_len, k_len, key_mask):

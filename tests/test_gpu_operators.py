@@ -729,3 +729,16 @@ def test_positions_beyond_64_bits_are_refused(kw):
                  lambda: vf.vf_qk_norm_rope_backward(x, x, x, 1, plan=plan, **kw)):
         with pytest.raises(vf.VfError):
             call()
+
+
+def test_attention_refuses_scales_and_empty_heads_on_the_device():
+    import torch
+    import paper_2009_09523_amd as vf
+    q, ws = torch.zeros(1, 2, 1, 64, device="cuda"), torch.empty(1 << 16, dtype=torch.uint8, device="cuda")
+    none, lse = torch.zeros(1, 2, 1, 0, device="cuda"), torch.zeros(1, 1, 2, device="cuda")
+    for x, scale in ((q, 1e39), (q, 0.0), (q, math.nan), (none, None)):
+        o, dq, dk, dv = (torch.empty_like(x) for _ in range(4))
+        for call in (lambda: vf.vf_attention(x, x, x, o, scale=scale, workspace=ws),
+                     lambda: vf.vf_attention_backward(x, x, x, x, lse, x, dq, dk, dv, scale=scale, workspace=ws)):
+            with pytest.raises(vf.VfError):
+                call()

@@ -246,3 +246,16 @@ def test_positions_that_float64_does_not_hold_are_refused(first):
     for call in (_rope, _norm, lambda **kw: _norm(True, **kw)):
         assert call(first=first) == EINVAL
     assert _rope(first=1 << 52, rows=0) == 0 and _norm(first=-(1 << 52), rows=0) == 0
+
+
+def test_scales_and_heads_that_the_attention_call_cannot_take_are_its_own_errors():
+    """No errors of the packing below: a scale beyond fp32, and the default scale of heads without elements."""
+    import torch
+    q = torch.zeros(1, 2, 1, 64)
+    for scale in (1e39, -1.0, 0.0, math.nan, math.inf):
+        with pytest.raises(vf.VfError) as e:
+            binding._ATTN_SHAPE.pack(*binding._attn_sizes("vf_attention", 1, q, q, q, scale), *range(24))
+        assert e.value.code == EINVAL
+    none = torch.zeros(1, 2, 1, 0)
+    s = binding.VfAttnShape.from_buffer_copy(binding._ATTN_SHAPE.pack(*binding._attn_sizes("vf_attention", 1, none, none, none, None), *range(24)))
+    assert vf.lib().vf_attention_workspace(C.byref(s), 0) == EINVAL
