@@ -463,7 +463,9 @@ int vf_attention_backward(const vf_attn_shape* shape, const void* q, const void*
                           const void* o, const float* lse, const void* d_o, void* dq, void* dk, void* dv,
                           void* workspace, int64_t workspace_bytes, void* stream);
 
-/* Bytes of workspace of the two calls above (backward = 0 / 1); VF_EINVAL (negative) for a malformed shape. */
+/* Bytes of workspace of the two calls above (backward = 0 / 1), whatever lengths and mask they are given; VF_EINVAL (negative) for a
+ * malformed shape.  0 for a forward call that takes the keys in one part, of up to 4096 keys; with more keys a call without key_mask
+ * is content with what remains without a bit for every key. */
 int64_t vf_attention_workspace(const vf_attn_shape* shape, int32_t backward);
 
 /* ---- training state of this device (Section 4.1) ---------------------------------------

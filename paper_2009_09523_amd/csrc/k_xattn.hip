@@ -1216,15 +1216,18 @@ static int by_width(int d_head, F f) {
   return d_head <= 96 ? f(std::integral_constant<int, 96>()) : f(std::integral_constant<int, 128>());
 }
 
-// The mask's bits; backward: two floats per row (lse and rowsum(dO o)); then the parts of one pass at a time.
+// The bits of a mask that no workgroup may have to make alone; backward: two floats per row (lse and rowsum(dO o)); then the parts of
+// one pass at a time.
 static int64_t mask_words(const vf_attn_shape& s) { return ((int64_t)s.k_rows + 63) / 64; }
-static int64_t mask_floats(const vf_attn_shape& s) { return round4(2 * s.batch * mask_words(s)); }
-int64_t attn_workspace_bytes(const vf_attn_shape& s, bool backward) {
+static int64_t mask_floats(const vf_attn_shape& s, bool masked) {
+  return masked && s.k_rows > kMaskWords * 64 ? round4(2 * s.batch * mask_words(s)) : 0;
+}
+int64_t attn_workspace_bytes(const vf_attn_shape& s, bool backward, bool masked) {
   if (!s.batch || (!backward && !s.q_rows)) return 0;
   const int64_t parts = part_rows_floats(s, split_rows(s, backward));
-  if (!backward) return (mask_floats(s) + parts) * (int64_t)sizeof(float);
+  if (!backward) return (mask_floats(s, masked) + parts) * (int64_t)sizeof(float);
   const int64_t stats = 2 * round4((int64_t)s.batch * s.q_heads * s.q_rows);
-  return (mask_floats(s) + stats + std::max(parts, part_keys_floats(s, split_keys(s)))) * (int64_t)sizeof(float);
+  return (mask_floats(s, masked) + stats + std::max(parts, part_keys_floats(s, split_keys(s)))) * (int64_t)sizeof(float);
 }
 
 static int make_bits(AttnJob& j, bool backward, float* ws, hipStream_t st) {
@@ -1243,7 +1246,7 @@ int launch_attn(AttnJob j, void* workspace, hipStream_t st) {
   if (!j.s.batch || !j.s.q_rows) return VF_OK;
   float* ws = static_cast<float*>(workspace);
   VF_TRY(make_bits(j, false, ws, st));
-  ws += mask_floats(j.s);
+  ws += mask_floats(j.s, j.key_mask);
   if (j.s.dtype == VF_BF16) return by_width<bf16_t>(j.s.d_head, [&](auto dp) { return pass_rows<bf16_t, decltype(dp)::value>(j, ws, false, st); });
   return by_width<float>(j.s.d_head, [&](auto dp) { return pass_rows<float, decltype(dp)::value>(j, ws, false, st); });
 }
@@ -1253,7 +1256,7 @@ int launch_attn_bwd(AttnJob j, void* workspace, hipStream_t st) {
   float* ws = static_cast<float*>(workspace);
   VF_TRY(make_bits(j, true, ws, st));
   const int64_t rows = round4((int64_t)j.s.batch * j.s.q_heads * j.s.q_rows);
-  j.row_lse = ws + mask_floats(j.s);
+  j.row_lse = ws + mask_floats(j.s, j.key_mask);
   j.row_delta = j.row_lse + rows;
   ws = j.row_delta + rows;
   if (j.s.dtype == VF_BF16) return by_width<bf16_t>(j.s.d_head, [&](auto dp) { return launch_bwd<bf16_t, decltype(dp)::value>(j, ws, st); });

@@ -590,7 +590,7 @@ struct AttnSplit {
   float* out[2];
   float* stats;
 };
-int64_t attn_workspace_bytes(const vf_attn_shape& s, bool backward);
+int64_t attn_workspace_bytes(const vf_attn_shape& s, bool backward, bool masked);
 int launch_attn(AttnJob j, void* workspace, hipStream_t st);
 int launch_attn_bwd(AttnJob j, void* workspace, hipStream_t st);
 

@@ -117,8 +117,8 @@ int make_job(const vf_attn_shape* s, const void* q, const void* k, const void* v
   return VF_OK;
 }
 
-int check_workspace(const vf_attn_shape& s, bool backward, const void* ws, int64_t bytes) {
-  const int64_t need = attn_workspace_bytes(s, backward);
+int check_workspace(const vf_attn_shape& s, bool backward, bool masked, const void* ws, int64_t bytes) {
+  const int64_t need = attn_workspace_bytes(s, backward, masked);
   return need > 0 && (!ws || !aligned16(ws) || bytes < need) ? VF_EINVAL : VF_OK;
 }
 
@@ -230,7 +230,7 @@ int vf_qk_norm_rope_backward(int32_t dtype, const void* x, int64_t x_row, int64_
 
 int64_t vf_attention_workspace(const vf_attn_shape* shape, int32_t backward) {
   VF_TRY(check_shape(shape));
-  return attn_workspace_bytes(*shape, backward != 0);
+  return attn_workspace_bytes(*shape, backward != 0, true);
 }
 
 int vf_attention(const vf_attn_shape* shape, const void* q, const void* k, const void* v, const int32_t* q_len,
@@ -242,7 +242,7 @@ int vf_attention(const vf_attn_shape* shape, const void* q, const void* k, const
   VF_TRY(make_job(shape, q, k, v, q_len, k_len, key_mask, &j));
   if (s.batch > 0 && s.q_rows > 0 && (!o || !aligned16(o))) return VF_EINVAL;
   if (!output_apart(s.o, s.batch, s.q_rows, s.q_heads, s.d_head) || (o && (o == q || o == k || o == v))) return VF_EINVAL;
-  VF_TRY(check_workspace(s, false, workspace, workspace_bytes));
+  VF_TRY(check_workspace(s, false, key_mask, workspace, workspace_bytes));
   j.o = o; j.lse = lse;
   return launch_attn(j, workspace, static_cast<hipStream_t>(stream));
 }
@@ -265,7 +265,7 @@ int vf_attention_backward(const vf_attn_shape* shape, const void* q, const void*
   for (int i = 0; i < 3; ++i)                               // (an output is read again, as an input, by other workgroups)
     for (const void* p : {q, k, v, o, d_o, static_cast<const void*>(outs[(i + 1) % 3])})
       if (outs[i] && outs[i] == p) return VF_EINVAL;
-  VF_TRY(check_workspace(s, true, workspace, workspace_bytes));
+  VF_TRY(check_workspace(s, true, key_mask, workspace, workspace_bytes));
   j.o = const_cast<void*>(o); j.lse = const_cast<float*>(lse);
   j.d_o = d_o; j.dq = dq; j.dk = dk; j.dv = dv;
   return launch_attn_bwd(j, workspace, static_cast<hipStream_t>(stream));

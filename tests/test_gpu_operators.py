@@ -742,3 +742,31 @@ def test_attention_refuses_scales_and_empty_heads_on_the_device():
                      lambda: vf.vf_attention_backward(x, x, x, x, lse, x, dq, dk, dv, scale=scale, workspace=ws)):
             with pytest.raises(vf.VfError):
                 call()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("B,Tq,Tk,Hq,Hk,dh", [(2, 40, 300, 2, 2, 64), (8, 512, 4500, 8, 8, 64)])
+def test_attention_without_a_workspace(B, Tq, Tk, Hq, Hk, dh, dtype):
+    """One part, no mask: nothing is needed, and the backward pass does without the mask's bits."""
+    import torch
+    import paper_2009_09523_amd as vf
+    g = torch.Generator(device="cuda").manual_seed(0)
+    q, do = (torch.randn(B, Tq, Hq, dh, generator=g, device="cuda").to(_t(dtype)) for _ in range(2))
+    k, v = (torch.randn(B, Tk, Hk, dh, generator=g, device="cuda").to(_t(dtype)) for _ in range(2))
+    runs, most = [], vf.vf_attention_workspace(q, k, v, backward=True)
+    bits = -(-B * -(-Tk // 64) * 8 // 16) * 16 if Tk > 4096 else 0
+    for space in (0, most):
+        o, lse, dq, dk, dv = torch.empty_like(q), torch.empty(B, Hq, Tq, device="cuda"), torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+        ws = torch.empty(space, dtype=torch.uint8, device="cuda") if space else None
+        vf.vf_attention(q, k, v, o, lse, workspace=ws)
+        vf.vf_attention_backward(q, k, v, o, lse, do, dq, dk, dv, workspace=torch.empty(space or most - bits, dtype=torch.uint8, device="cuda"))
+        runs.append((o, lse, dq, dk, dv))
+    for a, b in zip(*runs):
+        assert torch.equal(a, b)
+    ones = torch.ones(B, Tk, dtype=torch.bool, device="cuda")
+    if Tk > 4096:
+        with pytest.raises(vf.VfError):
+            vf.vf_attention(q, k, v, torch.empty_like(q), key_mask=ones)
+    else:
+        vf.vf_attention(q, k, v, o, lse, key_mask=ones)
+        assert torch.equal(o, runs[0][0])

@@ -259,3 +259,18 @@ def test_scales_and_heads_that_the_attention_call_cannot_take_are_its_own_errors
     none = torch.zeros(1, 2, 1, 0)
     s = binding.VfAttnShape.from_buffer_copy(binding._ATTN_SHAPE.pack(*binding._attn_sizes("vf_attention", 1, none, none, none, None), *range(24)))
     assert vf.lib().vf_attention_workspace(C.byref(s), 0) == EINVAL
+
+
+def test_only_calls_that_use_a_workspace_need_one():
+    """Bits of a long mask, and parts: the plainest forward call needs none."""
+    need = lambda s, b: vf.lib().vf_attention_workspace(C.byref(s), b)  # noqa: E731
+    short, long = _shape(batch=8, q_rows=512, k_rows=4096, q_heads=8, kv_heads=8), _shape(batch=8, q_rows=512, k_rows=4500, q_heads=8, kv_heads=8)
+    rows = 8 * 8 * 512 * 4
+    assert need(short, 0) == 0 and need(short, 1) == 2 * rows
+    bits = -(-8 * 71 * 8 // 16) * 16
+    assert need(long, 0) == bits and need(long, 1) == 2 * rows + bits
+
+    def forward(mask, ws, size):
+        return vf.lib().vf_attention(C.byref(long), P, P, P, None, None, mask, 2 * P, None, ws, size, None)
+    assert forward(3 * P, None, 0) == EINVAL and forward(3 * P, 4 * P, bits - 1) == EINVAL
+    assert _backward(long, bytes=2 * rows - 1) == EINVAL and _backward(long, ws=None, bytes=0) == EINVAL
