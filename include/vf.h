@@ -429,7 +429,10 @@ typedef struct vf_attn_layout {
 } vf_attn_layout;
 
 /* Attention of q_rows queries to k_rows keys and values.  Plain data, read on the host by the call.
- * Pointers 16-byte aligned; every stride a multiple of 16 bytes; d_head a multiple of 8, 8 .. 128. */
+ * Pointers 16-byte aligned; every stride a multiple of 16 bytes; d_head a multiple of 8, 8 .. 128.
+ * Sizes, with g = q_heads / kv_heads: g q_rows and k_rows up to 128 * 65535 = 8388480 (the query heads that share a key
+ * head are rows of one problem), batch * kv_heads up to 2^23, and g^2 q_rows and batch * kv_heads * max(g q_rows, k_rows) up to
+ * 2^31 - 1. */
 typedef struct vf_attn_shape {
   int32_t dtype;                     /* VF_F32 | VF_BF16, of all tensors but lse */
   int32_t batch, q_rows, k_rows;

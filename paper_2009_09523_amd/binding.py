@@ -443,7 +443,8 @@ def vf_attention_workspace(q, k, v, backward: bool = False) -> int:
 def vf_attention(q, k, v, o, lse=None, q_len=None, k_len=None, key_mask=None, scale=None, workspace=None, stream=None):
     """o = softmax(scale q k^T) v over the visible keys.  q, o: [batch, q_rows, q_heads, d_head]; k, v: [batch, k_rows,
     kv_heads, d_head]; lse: fp32 [batch, q_heads, q_rows] for the backward pass; q_len, k_len: int32 [batch]; key_mask:
-    uint8 or bool [batch, k_rows]; scale: 1 / sqrt(d_head) if None."""
+    uint8 or bool [batch, k_rows]; scale: 1 / sqrt(d_head) if None.  d_head: a multiple of 8 up to 128; with g = q_heads / kv_heads,
+    g q_rows and k_rows up to 8388480, batch * kv_heads up to 2^23, g^2 q_rows and batch * kv_heads * the longer side up to 2^31 - 1."""
     where = "vf_attention"
     t, dev, code, qs, ks, vs, os_ = _floats(where, q, k, v, o)
     sizes = _attn_sizes(where, code, q, k, v, scale)

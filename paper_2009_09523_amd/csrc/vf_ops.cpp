@@ -87,7 +87,8 @@ int check_shape(const vf_attn_shape* s) {
   // a grid, joined rows are counted in 32 bits
   const int64_t group = s->q_heads / s->kv_heads, problems = (int64_t)s->batch * s->kv_heads;
   const int64_t rows = std::max<int64_t>(group * s->q_rows, s->k_rows);
-  if (group * group * s->q_rows > INT32_MAX || rows > 128 * 65535 || problems > (1 << 23) || problems * rows > INT32_MAX) return VF_EINVAL;
+  if (rows > 128 * 65535 || problems > (1 << 23)) return VF_EINVAL;       // (ahead of the products below, which then fit 64 bits)
+  if (group * group * s->q_rows > INT32_MAX || problems * rows > INT32_MAX) return VF_EINVAL;
   return VF_OK;
 }
 

@@ -770,3 +770,102 @@ def test_attention_without_a_workspace(B, Tq, Tk, Hq, Hk, dh, dtype):
     else:
         vf.vf_attention(q, k, v, o, lse, key_mask=ones)
         assert torch.equal(o, runs[0][0])
+
+
+def _small_ints(g, lo, hi, dtype, *shape):
+    import torch
+    return torch.randint(lo, hi + 1, shape, generator=g, device="cuda").to(_t(dtype))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_largest_number_of_rows_to_a_problem(dtype):
+    """65535 queries of 128 heads that share four keys, in whole numbers: scores of 0, weights of 1/4, values 0 to 3, o of 3/2, and sums of
+    8388480 rows whose terms are of one sign."""
+    import torch
+    import paper_2009_09523_amd as vf
+    T, H, dh = 65535, 128, 8
+    g = torch.Generator(device="cuda").manual_seed(5)
+    q, do = _small_ints(g, 0, 1, dtype, 1, T, H, dh), _small_ints(g, 0, 2, dtype, 1, T, H, dh)
+    k, v = torch.zeros(1, 4, 1, dh, device="cuda", dtype=_t(dtype)), torch.arange(4, device="cuda").to(_t(dtype))[None, :, None, None].expand(1, 4, 1, dh).contiguous()
+    o, lse, dq, dk, dv = torch.empty_like(q), torch.empty(1, H, T, device="cuda"), torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    ws = torch.empty(vf.vf_attention_workspace(q, k, v, backward=True), dtype=torch.uint8, device="cuda")
+    vf.vf_attention(q, k, v, o, lse, scale=0.5, workspace=ws)
+    vf.vf_attention_backward(q, k, v, o, lse, do, dq, dk, dv, scale=0.5, workspace=ws)
+    assert (o == 1.5).all() and (dq == 0).all()
+    assert ((lse.double() - math.log(4)).abs() <= 8 * E).all()
+    dd, qq = do.double().view(-1, dh), q.double().view(-1, dh)
+    # dz = (key - 3/2) / 4 times the sum of dO, multiples of 1/8 up to 6
+    dz = 0.25 * (torch.arange(4, device="cuda").double() - 1.5) * dd.sum(1, keepdim=True)
+    # p = exp(0 - lse) and the exact rowsum leave 16 roundings, which bf16 operands (of up to 8 bits here) do not see; the rows go in
+    # 64 parts, 16 (fp32: 2) to an instruction: additions one behind the other, and the rows of an instruction and the parts
+    chain = 8388480 / 64 / (16 if dtype == BF16 else 2) + 128
+    for got, want in ((dv, 0.25 * dd.sum(0).expand(4, dh)), (dk, 0.5 * dz.T @ qq)):
+        _close(got[0, :, 0], want.cpu(), want.cpu().abs() * ((chain + 32) * E + _u(dtype)), "gradients")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_largest_number_of_keys(dtype):
+    """One query and 8388480 keys of which a mask leaves the last 2^22: weights of 2^-22, whole values, sums below 2^24."""
+    import torch
+    import paper_2009_09523_amd as vf
+    T, n, dh = 8388480, 1 << 22, 8
+    g = torch.Generator(device="cuda").manual_seed(6)
+    q, do = _small_ints(g, -1, 1, dtype, 1, 1, 1, dh), _small_ints(g, -2, 2, dtype, 1, 1, 1, dh)
+    k, v = torch.zeros(1, T, 1, dh, device="cuda", dtype=_t(dtype)), _small_ints(g, -1, 2, dtype, 1, T, 1, dh)
+    mask = torch.arange(T, device="cuda")[None] >= T - n
+    o, lse, dq, dk, dv = torch.empty_like(q), torch.empty(1, 1, 1, device="cuda"), torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    ws = torch.empty(vf.vf_attention_workspace(q, k, v, backward=True), dtype=torch.uint8, device="cuda")
+    vf.vf_attention(q, k, v, o, lse, key_mask=mask, workspace=ws)
+    vf.vf_attention_backward(q, k, v, o, lse, do, dq, dk, dv, key_mask=mask, workspace=ws)
+    want = (v[0, T - n:, 0].double().sum(0) / n).cpu()
+    _close(o[0, 0, 0], want, want.abs() * (4 * E + _u(dtype)), "o")
+    assert abs(float(lse) - 22 * math.log(2)) <= 4 * E * 22 and (dq == 0).all()
+    assert (dv[0, :T - n] == 0).all() and (dk[0, :T - n] == 0).all() and dk.isfinite().all()
+    # p from the stored logarithm: two roundings of 22 in the exponent, three in the logarithm and the exponential
+    want = (do[0, 0].double() / n).cpu().expand(n, dh)
+    _close(dv[0, T - n:, 0], want, want.abs() * (64 * E + _u(dtype)), "dv")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_largest_number_of_problems(dtype):
+    """2^23 samples of one query and one key: every output is the value, and every score's gradient is 0."""
+    import torch
+    import paper_2009_09523_amd as vf
+    B, dh = 1 << 23, 8
+    g = torch.Generator(device="cuda").manual_seed(7)
+    q, k, v, do = (_small_ints(g, -2, 2, dtype, B, 1, 1, dh) for _ in range(4))
+    o, lse, dq, dk, dv = torch.empty_like(q), torch.empty(B, 1, 1, device="cuda"), torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    ws = torch.empty(vf.vf_attention_workspace(q, k, v, backward=True), dtype=torch.uint8, device="cuda")
+    vf.vf_attention(q, k, v, o, lse, workspace=ws)
+    vf.vf_attention_backward(q, k, v, o, lse, do, dq, dk, dv, workspace=ws)
+    z = (q.double() * k.double()).sum(-1)[:, 0, 0] * dh ** -0.5
+    assert ((lse.view(-1).double() - z).abs() <= 8 * E * (z.abs() + 1)).all()
+    # scores of up to 12: p = exp(z - lse) is 1 within 64 roundings; o is p v / p, off by 4 roundings, so dp - rowsum(dO o), whose terms sum
+    # up to 32, by 4 * 32, the exact rowsum by as much again, and dq and dk by 2 / sqrt(8) of that.  bf16 sees none of it
+    f32 = dtype == F32
+    assert ((o.double() - v.double()).abs() <= (4 * E if f32 else 0.0) * v.double().abs()).all()
+    assert ((dv.double() - do.double()).abs() <= (64 * E if f32 else 0.0) * do.double().abs()).all()
+    assert (dq.double().abs() <= (256 * E if f32 else 0.0)).all() and (dk.double().abs() <= (256 * E if f32 else 0.0)).all()
+
+
+def test_largest_number_of_rows_of_the_rotation_and_norm():
+    """2^31 - 1 rows of one short head: first and last rows and some between, rotation, norm, and the norm's gradient."""
+    import torch
+    import paper_2009_09523_amd as vf
+    rows, dh, seq = (1 << 31) - 1, 2, 1000
+    g = torch.Generator(device="cuda").manual_seed(8)
+    piece = torch.randn(1 << 20, 1, dh, generator=g, device="cuda").to(torch.bfloat16)
+    x = piece.repeat(2048, 1, 1)[:rows]
+    some = torch.cat([torch.arange(300), torch.randint(0, rows, (2000,), generator=torch.Generator().manual_seed(9)), rows - 1 - torch.arange(300)])
+    at = some.cuda()
+    xs, dys = x[at].double().cpu(), x[at].double().cpu()
+    pos, plan, one = some % seq + 5, _plan(vf, dh, "half"), torch.ones(dh, dtype=torch.float64)
+    y = torch.empty_like(x)
+    vf.vf_rope(x, y, plan, first=5, seq_len=seq)
+    want, mag = _turn(xs, pos, dh, "half", _freqs(dh), 1.0)
+    _close(y[at], want, mag * TURN + 2.0 ** -8 * want.abs(), "rotation")
+    ref = _norm_ref(xs, dys, 1, one, one, float(np.float32(1e-6)), pos, dh, "half")
+    vf.vf_qk_norm_rope(x, y, 1, plan=plan, first=5, seq_len=seq)
+    _close(y[at], ref["y"][0], ref["y"][1] * 40 * E + 2.0 ** -8 * ref["y"][0].abs(), "norm")
+    vf.vf_qk_norm_rope_backward(x, x, y, 1, plan=plan, first=5, seq_len=seq)
+    _close(y[at], ref["dx"][0], ref["dx"][1] * 120 * E + 2.0 ** -8 * ref["dx"][0].abs(), "gradient")

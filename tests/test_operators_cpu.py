@@ -274,3 +274,21 @@ def test_only_calls_that_use_a_workspace_need_one():
         return vf.lib().vf_attention(C.byref(long), P, P, P, None, None, mask, 2 * P, None, ws, size, None)
     assert forward(3 * P, None, 0) == EINVAL and forward(3 * P, 4 * P, bits - 1) == EINVAL
     assert _backward(long, bytes=2 * rows - 1) == EINVAL and _backward(long, ws=None, bytes=0) == EINVAL
+
+
+@pytest.mark.parametrize("fits,beyond", [
+    (dict(batch=1, q_heads=128, kv_heads=1, q_rows=65535), dict(q_rows=65536)),                   # rows of a problem: 8388480
+    (dict(batch=1, q_heads=1, kv_heads=1, q_rows=8388480), dict(q_rows=8388481)),
+    (dict(batch=1, q_heads=1, kv_heads=1, k_rows=8388480), dict(k_rows=8388481)),
+    (dict(batch=1 << 23, q_heads=1, kv_heads=1, q_rows=1, k_rows=1), dict(batch=(1 << 23) + 1)),
+    (dict(batch=1 << 20, q_heads=8, kv_heads=8, q_rows=1, k_rows=1), dict(batch=(1 << 20) + 1)),
+    (dict(batch=1, q_heads=1024, kv_heads=1, q_rows=2047), dict(q_rows=2048)),                    # 1024^2 rows: 2^31
+    (dict(batch=4096, q_heads=1, kv_heads=1, q_rows=1, k_rows=524287), dict(k_rows=524288)),
+    (dict(batch=4096, q_heads=4, kv_heads=1, q_rows=131071, k_rows=1), dict(q_rows=131072)),
+    (dict(batch=1, q_heads=1, kv_heads=1), dict(q_heads=(1 << 31) - 1, q_rows=(1 << 31) - 1)),    # products beyond 64 bits
+])
+def test_largest_attention_that_is_taken(fits, beyond):
+    for backward in (0, 1):
+        assert vf.lib().vf_attention_workspace(C.byref(_shape(**fits)), backward) >= 0
+        assert vf.lib().vf_attention_workspace(C.byref(_shape(**(fits | beyond))), backward) == EINVAL
+    assert _forward(_shape(**(fits | beyond))) == EINVAL and _backward(_shape(**(fits | beyond))) == EINVAL
