@@ -869,3 +869,56 @@ def test_largest_number_of_rows_of_the_rotation_and_norm():
     _close(y[at], ref["y"][0], ref["y"][1] * 40 * E + 2.0 ** -8 * ref["y"][0].abs(), "norm")
     vf.vf_qk_norm_rope_backward(x, x, y, 1, plan=plan, first=5, seq_len=seq)
     _close(y[at], ref["dx"][0], ref["dx"][1] * 120 * E + 2.0 ** -8 * ref["dx"][0].abs(), "gradient")
+
+
+def _exact_rowsum_ref(q, k, v, do, scale, o_dev):
+    """dq and dk in float64 with bounds that leave no room for what rounding o puts into rowsum(dO o), and what they would be with it.
+
+    The dq kernel starts from e = rowsum(dO (o' - o)) off; its dz = p (dp - rowsum) - p e sum up to rest = -e, which it takes out again.
+    What stays: a rounding of dz - p e and (dq) of the p that -rest is spread by; the fp32 errors of dp, the rowsum and the sums."""
+    import torch
+    u, G = 2.0 ** -8, q.shape[2] // k.shape[2]
+    dh = q.shape[3]
+    dq, dqb, dqw = (torch.zeros(q.shape, dtype=torch.float64) for _ in range(3))
+    dk, dkb, dkw = (torch.zeros(k.shape, dtype=torch.float64) for _ in range(3))
+    for b in range(q.shape[0]):
+        for h in range(q.shape[2]):
+            qq, kk, vv, dd = q[b, :, h], k[b, :, h // G], v[b, :, h // G], do[b, :, h]
+            n = len(kk)
+            z = scale * qq @ kk.T
+            rel = (2 * (dh + 4) * float((scale * qq.abs() @ kk.abs().T).max()) + 2 * n + 16) * E         # of p, as in the reference above
+            p = torch.softmax(z, 1)
+            o = p @ vv
+            e = (dd * (o_dev[b, :, h] - o)).sum(1, keepdim=True)
+            dp, delta = dd @ vv.T, (dd * o).sum(1, keepdim=True)
+            dz = p * (dp - delta)
+            first = dz.abs() + p * e.abs()
+            fp32 = (dd.abs() @ vv.abs().T + (dd.abs() * o.abs()).sum(1, keepdim=True)) * (dh + 4) * E
+            rest = (p * fp32 + first * (rel + n * E)).sum(1, keepdim=True)                              # error of rest
+            zq = first * (u + rel + n * E) + p * (fp32 + rest + e.abs() * (u + rel + n * E))
+            zk = dz.abs() * (u + rel + len(qq) * G * E) + p * (fp32 + rest) * (1 + u)
+            g = scale * dz @ kk
+            dq[b, :, h], dqb[b, :, h], dqw[b, :, h] = g, scale * zq @ kk.abs() * 1.01 + u * g.abs(), g - scale * (p * e) @ kk
+            dk[b, :, h // G] += scale * dz.T @ qq
+            dkb[b, :, h // G] += scale * zk.T @ qq.abs() * 1.01
+            dkw[b, :, h // G] += scale * (dz - p * e).T @ qq
+    return (dq, dqb, dqw), (dk, dkb + u * dk.abs(), dkw)
+
+
+# exact dq: four wavefronts to a block of rows (heads of 80, 128), two (128), one (64, 128; dk/dv in parts); dk alone: keys in parts
+@pytest.mark.parametrize("B,Tq,Tk,Hq,Hk,dh,exact", [(1, 200, 77, 4, 4, 80, True), (4, 40, 300, 8, 4, 128, True), (32, 33, 257, 8, 8, 128, True),
+                                                    (16, 260, 90, 8, 8, 64, True), (2, 9, 120, 4, 4, 128, True), (1, 1030, 9, 2, 2, 64, True),
+                                                    (1, 40, 6000, 2, 2, 96, False), (2, 4, 9000, 4, 2, 64, False)])
+def test_gradients_without_the_rounding_of_o(B, Tq, Tk, Hq, Hk, dh, exact):
+    """Values far from 0, whose o is rounded by more than they differ, beside keys far from 0: left in the rowsum, that rounding is most of
+    the error of dq and dk.  Rows of a head repeat, so that it does not cancel in dk."""
+    q, k, v, do = _inputs(B, Tq, Tk, Hq, Hk, dh, BF16)
+    q, do = (0.3 * q[:, :1]).expand(q.shape).contiguous(), do[:, :1].expand(do.shape).contiguous()
+    q, k, v, do = (t.to(_t(BF16)).double() for t in (q, 8 + k, 64 + 2 * v, do))
+    got = _attend(q, k, v, do, BF16)
+    refs = _exact_rowsum_ref(q, k, v, do, dh ** -0.5, got["o"].double().cpu())
+    for name, (want, bound, with_it) in zip(("dq", "dk"), refs):
+        if name == "dq" and not exact:
+            continue
+        assert float(((with_it - want).abs() > bound).double().mean()) > 0.1, name       # such an error would not pass
+        _close(got[name], want, bound, name)
