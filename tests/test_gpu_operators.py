@@ -922,3 +922,104 @@ def test_gradients_without_the_rounding_of_o(B, Tq, Tk, Hq, Hk, dh, exact):
             continue
         assert float(((with_it - want).abs() > bound).double().mean()) > 0.1, name       # such an error would not pass
         _close(got[name], want, bound, name)
+
+
+def _inside(t, before, behind, between=0):
+    """t's rows and heads inside wider rows of NaN: `before` and `behind` elements around a row, `between` behind every head."""
+    import torch
+    rows, heads, dh = t.shape
+    wide = torch.full((rows, before + heads * (dh + between) + behind), math.nan, dtype=t.dtype, device=t.device)
+    view = wide.as_strided((rows, heads, dh), (wide.stride(0), dh + between, 1), before)
+    view.copy_(t)
+    return wide, view
+
+
+# what lies around a row and between its heads: 16-byte chunks everywhere, in x alone, nowhere (odd addresses; odd strides of heads)
+PLACES = [((8, 24, 0), (0, 8, 8), (16, 0, 16)), ((8, 8, 0), (3, 5, 0), (0, 0, 0)), ((1, 2, 0), (2, 1, 0), (5, 6, 0)), ((0, 0, 1), (0, 3, 3), (7, 0, 5))]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rot,layout", [(64, "half"), (24, "interleaved"), (20, "half"), (0, "half")])
+@pytest.mark.parametrize("places", PLACES)
+def test_norm_of_heads_inside_wider_rows(places, rot, layout, dtype):
+    """x, y (dx) and dy each with strides of its own; what lies around the outputs stays."""
+    import torch
+    import paper_2009_09523_amd as vf
+    rows, hq, hk, dh = 37, 3, 2, 64
+    x, dy = _randn(21, rows, hq + hk, dh, dtype=dtype), _randn(22, rows, hq + hk, dh, dtype=dtype, scale=0.1)
+    gq, gk = (1 + 0.2 * _randn(s, dh, dtype=F32).float().double() for s in (23, 24))
+    gq, gk = gq.float().double(), gk.float().double()
+    xw, xv = _inside(_dev(x, dtype), *places[0])
+    dw, dv = _inside(_dev(dy, dtype), *places[1])
+    plan = _plan(vf, rot, layout) if rot else None
+    ref = _norm_ref(x, dy, hq, gq, gk, float(np.float32(1e-6)), torch.arange(rows) + 9, rot, layout)
+    norm, u = (0.5 * 24 + 8) * E, _u(dtype) if dtype == BF16 else 0.0            # as above
+    kw = dict(plan=plan, first=9)
+    yw, yv = _inside(torch.zeros_like(xv), *places[2])
+    vf.vf_qk_norm_rope(xv, yv, hq, gq.float().cuda(), gk.float().cuda(), **kw)
+    _close(yv, ref["y"][0], ref["y"][1] * (norm + TURN) + u * ref["y"][0].abs(), "y")
+    dgq, dgk = torch.empty(dh, device="cuda"), torch.empty(dh, device="cuda")
+    ws = torch.empty(vf.vf_qk_norm_rope_workspace(rows, hq, hk, dh), dtype=torch.uint8, device="cuda")
+    gw, gv = _inside(torch.zeros_like(xv), *places[2])
+    vf.vf_qk_norm_rope_backward(xv, dv, gv, hq, gq.float().cuda(), gk.float().cuda(), dgq, dgk, ws, **kw)
+    _close(gv, ref["dx"][0], ref["dx"][1] * (3 * norm + TURN + 32 * E) + u * ref["dx"][0].abs(), "dx")
+    for name, got in (("dgamma_q", dgq), ("dgamma_k", dgk)):
+        want, mag = ref[name]
+        _close(got, want, mag * (512 * E + norm + TURN), name)
+    for wide, view in ((yw, yv), (gw, gv)):
+        view.fill_(math.nan)
+        assert wide.isnan().all()
+    if rot:
+        yw, yv = _inside(torch.zeros_like(xv), *places[2])
+        vf.vf_rope(xv, yv, plan, first=9)
+        want, mag = _turn(x, torch.arange(rows) + 9, rot, layout, _freqs(rot), 1.0)
+        _close(yv, want, mag * TURN + u * want.abs(), "rotation")
+        yv.fill_(math.nan)
+        assert yw.isnan().all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_norm_of_repeated_and_turned_round_tensors(dtype):
+    """Heads ahead of rows in memory, and one row or head read for all (stride 0) of x and dy."""
+    import torch
+    import paper_2009_09523_amd as vf
+    rows, hq, hk, dh = 29, 2, 3, 40
+    gq, gk = torch.ones(dh, dtype=torch.float64), torch.full((dh,), 0.5, dtype=torch.float64)
+    norm, u = (0.5 * 24 + 8) * E, _u(dtype) if dtype == BF16 else 0.0
+    plan = _plan(vf, dh, "half")
+    for kind in ("heads first", "one row", "one head"):
+        x, dy = _randn(31, rows, hq + hk, dh, dtype=dtype), _randn(32, rows, hq + hk, dh, dtype=dtype, scale=0.1)
+        if kind == "heads first":
+            xd, dd = (_dev(t, dtype).transpose(0, 1).contiguous().transpose(0, 1) for t in (x, dy))
+        else:
+            one = (lambda t: t[:1]) if kind == "one row" else (lambda t: t[:, :1])
+            xd, dd = (_dev(one(t), dtype).expand(rows, hq + hk, dh) for t in (x, dy))
+            x, dy = (one(t).expand(rows, hq + hk, dh) for t in (x, dy))
+        ref = _norm_ref(x, dy, hq, gq, gk, float(np.float32(1e-6)), torch.arange(rows), dh, "half")
+        y, dx = (torch.empty(hq + hk, rows, dh, dtype=_t(dtype), device="cuda").transpose(0, 1) for _ in range(2))
+        vf.vf_qk_norm_rope(xd, y, hq, None, gk.float().cuda(), plan=plan)
+        vf.vf_qk_norm_rope_backward(xd, dd, dx, hq, None, gk.float().cuda(), plan=plan)
+        _close(y, ref["y"][0], ref["y"][1] * (norm + TURN) + u * ref["y"][0].abs(), kind)
+        _close(dx, ref["dx"][0], ref["dx"][1] * (3 * norm + TURN + 32 * E) + u * ref["dx"][0].abs(), kind)
+
+
+@pytest.mark.parametrize("Tk", [70, 4500])
+def test_truth_values_as_a_key_mask(Tk):
+    """bool and uint8 masks are one; any value but 0 counts as visible."""
+    import torch
+    import paper_2009_09523_amd as vf
+    q, k, v, do = (_dev(t, BF16) for t in _inputs(2, 5, Tk, 2, 2, 64, BF16))
+    mask = torch.from_numpy(np.random.Generator(np.random.PCG64(3)).random((2, Tk)) < 0.5).cuda()
+    ws = torch.empty(max(1, vf.vf_attention_workspace(q, k, v, backward=True)), dtype=torch.uint8, device="cuda")
+    runs = []
+    for m in (mask, mask.to(torch.uint8), mask.to(torch.uint8) * 0x40):
+        out = [torch.empty_like(q), torch.empty(2, 2, 5, device="cuda"), torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)]
+        vf.vf_attention(q, k, v, out[0], out[1], key_mask=m, workspace=ws)
+        vf.vf_attention_backward(q, k, v, out[0], out[1], do, *out[2:], key_mask=m, workspace=ws)
+        runs.append(out)
+    for other in runs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(runs[0], other))
+    assert (runs[0][3][~mask] == 0).all() and (runs[0][3][mask] != 0).any()
+    for bad in (mask.t().contiguous().t(), mask[:, :-1], mask.int()):
+        with pytest.raises(vf.VfError):
+            vf.vf_attention(q, k, v, runs[0][0], key_mask=bad, workspace=ws)
