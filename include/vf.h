@@ -353,7 +353,9 @@ int vf_gemm_noalloc(const void* A, int64_t lda, const void* B, int64_t ldb, floa
  *     calls on different streams do not disturb each other as long as each has its own workspace.
  *     Calls may be captured into a HIP graph; a workspace belongs to the graph then;
  *   - the results of a call do not depend on what runs beside it: sums are taken in a fixed order,
- *     without atomics;
+ *     without atomics.  That order goes by the call's sizes: where a sample is one of another number
+ *     of samples, vf_attention may share its keys among wavefronts and parts in another way, and its
+ *     results (and dgamma of the norm) agree up to the roundings of fp32 sums, not bit by bit;
  *   - a call over no rows is a no-op (gradients that sum over the rows are then 0);
  *   - VF_EINVAL, with nothing enqueued, for malformed arguments. */
 
@@ -399,7 +401,7 @@ int vf_rope(int32_t dtype, const void* x, int64_t x_row, int64_t x_head, void* y
             int64_t first, int64_t seq_len, const vf_rope_plan* plan, int32_t inverse, void* stream);
 
 /* RMS norm of every head and the rotation in one pass:  y = R(x rstd gamma),
- * rstd = (mean over the head of x^2 + eps)^(-1/2), rounded once.  x, y: [rows, q_heads + k_heads, d_head] (as the
+ * rstd = (mean over the head of x^2 + eps)^(-1/2), rounded once; the sum of the squares has to stay within fp32.  x, y: [rows, q_heads + k_heads, d_head] (as the
  * projection writes them side by side; either number may be 0 for tensors of their own).
  * gamma_q, gamma_k: device fp32 [d_head], the weights of the first q_heads and the last k_heads heads
  * (NULL = all ones).  plan: NULL = the norm alone.  Positions as in vf_rope.  y may be x. */
@@ -443,7 +445,7 @@ typedef struct vf_attn_shape {
   vf_attn_layout d_o, dq, dk, dv;    /* backward only: gradient of o (input), of q, k, v (outputs) */
 } vf_attn_shape;
 
-/* o = softmax_keys(scale q k^T over the visible keys) v.
+/* o = softmax_keys(scale q k^T over the visible keys) v.  Every row sees the same keys of its sample: there is no causal mask.
  *   q_len     device int32 [batch] or NULL: rows from q_len[b] on are padding (values clamped into [0, q_rows])
  *   k_len     device int32 [batch] or NULL: keys from k_len[b] on are not visible (clamped into [0, k_rows])
  *   key_mask  device uint8 [batch, k_rows] or NULL: keys with a 0 are not visible
@@ -451,7 +453,8 @@ typedef struct vf_attn_shape {
  *             visible scaled products, which the backward pass needs
  * A row that is padding or sees no key has output 0 and lse -infinity.  What lies in padded rows and
  * invisible keys and values, infinities and NaN among it, has no influence.  Sums and softmax are fp32; with VF_BF16
- * the probabilities are rounded to bf16 as operands of the product with v.
+ * the probabilities are rounded to bf16 as operands of the product with v: o is off by 0.0023 to 0.0024 of its
+ * norm, where one rounding at the end leaves 0.0017.
  * workspace: device, 16-byte aligned, at least vf_attention_workspace(shape, 0) bytes. */
 int vf_attention(const vf_attn_shape* shape, const void* q, const void* k, const void* v,
                  const int32_t* q_len, const int32_t* k_len, const uint8_t* key_mask, void* o, float* lse,
@@ -459,7 +462,11 @@ int vf_attention(const vf_attn_shape* shape, const void* q, const void* k, const
 
 /* Gradients of q, k and v from d_o, the gradient of o; o and lse as the forward call wrote them, the
  * same lengths and mask.  Gradients of padded rows and invisible keys are 0; those of shared
- * keys and values are summed over the query heads that read them.
+ * keys and values are summed over the query heads that read them.  Sums are fp32.  With VF_BF16 the probabilities p and
+ * the gradients of the scores are rounded to bf16 as operands of the products with d_o, k and q, and o was rounded before
+ * rowsum(d_o o) is taken from it.  dk is free of that last rounding; dq is so for sources of up to 2048 keys (512
+ * where d_head is above 96) that go in one part, and otherwise off by scale e sum_keys(p k), with e the rounding's share of the
+ * row's rowsum: little beside the other roundings unless the keys share a large offset.
  * workspace: at least vf_attention_workspace(shape, 1) bytes. */
 int vf_attention_backward(const vf_attn_shape* shape, const void* q, const void* k, const void* v,
                           const int32_t* q_len, const int32_t* k_len, const uint8_t* key_mask,

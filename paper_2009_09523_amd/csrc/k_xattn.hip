@@ -456,8 +456,10 @@ __device__ __forceinline__ void remove(f32x16 (&a)[N], const f32x16 (&b)[N], flo
 #pragma unroll
     for (int r = 0; r < 16; ++r) a[i][r] = fmaf(-f, b[i][r], a[i][r]);
 }
-// Wavefronts to a SIMD that the kernels' registers are kept down to: two wherever that spills nothing (next to nothing in
-// the dq kernel with four wavefronts to a block at fp32 of 64 and bf16 of 128), else one.
+// Wavefronts to a SIMD that the kernels' registers are kept down to: two wherever that spills no vector register, else one.  Two
+// exceptions, both dq with four wavefronts to a block: bf16 of 128, not exact, spills 26 registers (2 x 4 x 9000 x 4 (2) x 128, backward:
+// 41.1 us, with one wavefront 39.9; 20 x 8000 x 8 x 128: 45.1 and 44.7), fp32 of 64 has 58 scalar registers in vector ones (9 x 64 x 211 x 4 x 64:
+// 29.7 us, with one 30.5; 4 x 40 x 1000 x 8 x 64: 40.1 and 40.8).
 template <typename T, int DP> constexpr int fwd_waves() { return DP * sizeof(T) <= 384 ? 2 : 1; }
 template <typename T, int DP, int SW, bool EXACT> constexpr int dq_waves() {
   return sizeof(T) == 4 ? (DP <= 64 ? 2 : 1) : !EXACT || DP <= 64 || (DP <= 96 && SW < 4) ? 2 : 1;
@@ -679,7 +681,7 @@ __global__ __launch_bounds__(NT, (fwd_waves<T, DP>())) void xattn_fwd_kernel(Att
 // ---- backward: dq, and lse / rowsum(dO o) of every row for the kernel behind it ---------------------
 // rowsum(dO o) from the rounded o is off by e, and every dz by -p e: their sum, which should be 0, is -e.  The kernel behind is
 // given the exact rowsum.  Here dq is off by -scale e sum(p k): nothing beside the rounding of dz when many keys share a
-// row and o is small, but a third of the error at 77 keys (0.0027 of the norm, 0.0023 without it).  EXACT takes sum(p k) along and
+// row and o is small, but 0.0014 of the norm at 77 keys (0.0027 in all, 0.0023 without it).  EXACT takes sum(p k) along and
 // removes it; for sources of up to 2048 keys (heads of more than 96 elements, where its registers cost the second wavefront of a
 // SIMD: 512), not in parts.
 template <typename T, int DP, int SW, bool EXACT>
@@ -1058,12 +1060,18 @@ __global__ __launch_bounds__(NT) void xattn_join_kernel(AttnJob j, AttnSplit sp,
 // quarter or half of a tile's blocks), and into parts, whose results a kernel behind joins.  Both make more and shorter workgroups
 // where few rows are held.  The choice is the one with the least estimated time, in us:
 //   a workgroup alone takes kStart + tiles * chain (its steps wait for each other), and as many of them run side by side as LDS and
-//   registers allow (`beside` to a compute unit);  workgroups of one compute unit share its matrix units: tiles * busy each.
+//   the forward kernel's registers allow (`beside` to a compute unit);  workgroups of one compute unit share its matrix units: tiles *
+//   busy each.
 //   Joining the wavefronts' results takes 1 us for 64 elements, parts cost kJoin and a pass over their fp32 results.
 // Measured per tile (forward): bf16 heads of 64: 1.1 chain, 0.55 busy (one block of 32 rows to a wavefront instead of two: 0.75, 0.3),
 // of 128: 1.8 and 1.15; fp32, bound by its matrix instructions: 2.4 and 2.1 at 64.  (192 workgroups of 7 tiles in three parts: 12.6 us
 // became 11.8 + 8.4; 256 workgroups of 24 tiles with sw = 4 instead of 1: 30 us became 19; 256 of 4 tiles, 128 wide: 13 us with
 // sw = 1, 15 with 2, 31 with 4.)
+// Of the other kernels, dk/dv of more than 128 bytes to a head and the fp32 dq of 96 have registers for one workgroup to a unit, and
+// so has the exact dq above 96 elements, which alone is counted so (`alone`), also where its keys then go in parts and the other dq
+// runs.  Counting one for each that has room for one changes the choice at 32 of 600 sizes (1 to 4096 queries, 1 to 8192 keys): backward
+// passes of fp32 up to 11 % slower (18 x 106 x 2202 x 6 (3) x 80: 407 -> 451 us), 6 % faster at one; of bf16 up to 14 % faster where
+// it takes fewer wavefronts to a block (39 x 1468 x 1319 x 2 x 80: 388 -> 332) and up to 15 % slower where more (56 x 711 x 59 x 5 x 96: 86 -> 99).
 constexpr int kUnits = 256, kMaxParts = 64;
 constexpr float kStart = 5.f, kJoin = 8.f;
 AttnSplit split_of(const vf_attn_shape& s, int held, int streamed, float work, bool alone) {
