@@ -467,6 +467,7 @@ int vf_attention(const vf_attn_shape* shape, const void* q, const void* k, const
  * rowsum(d_o o) is taken from it.  dk is free of that last rounding; dq is so for sources of up to 2048 keys (512
  * where d_head is above 96) that go in one part, and otherwise off by scale e sum_keys(p k), with e the rounding's share of the
  * row's rowsum: little beside the other roundings unless the keys share a large offset.
+ * Probabilities are taken again from lse, whose rounding they multiply: off by some 2^-23 |lse| of themselves.
  * workspace: at least vf_attention_workspace(shape, 1) bytes. */
 int vf_attention_backward(const vf_attn_shape* shape, const void* q, const void* k, const void* v,
                           const int32_t* q_len, const int32_t* k_len, const uint8_t* key_mask,
